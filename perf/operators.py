@@ -1,0 +1,480 @@
+"""The operators around the 8-bit key/value cache: what a serving program calls in a layer, one call
+at a time - norm and rotation of a step's queries and keys, the quantising writes, the read-back and
+the attention that reads the stored form.
+
+Stored form: a row (one token, one head, K or V) of head_dim values is one exponent e and head_dim
+e4m3 codes; e is the smallest integer with amax <= 448 * 2^e over the row's finite values, held in
+[-60, 60], and a code is value * 2^-e rounded to nearest even.  A page is, head after head,
+[K codes][V codes][K exponents + 127][V exponents + 127]; codes lie in sub-blocks of 16 tokens,
+    K: [dims / g][16 tokens][g dims]              with g = min(16, head_dim / 4)
+    V: [dims / 4g][4 groups of 4 tokens][16 dims][g / 4 sixteens of dims][4 tokens].
+
+A case fixes shapes and lengths (drawn from its own `shape` number); the seed of `prepare` fixes block
+tables and values.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+DEVICE = "cuda:0"
+CHUNK = 1024            # tokens of a host chunk, the granularity of restores
+POOL_FACTOR = 1.25      # pool pages per demanded page: a user's pages lie scattered
+
+
+def _case(name=None, **kw):
+    c = dict(
+        kind="attend",          # "attend", "write" (and read back), "read", "rotate"
+        dtype="bf16",           # of the rows: queries, keys, values, outputs
+        kv_heads=8, group=1,    # key heads, query heads that share one
+        head_dim=64, page=16,
+        users=1, prefix_lo=256, prefix_hi=256, prefix_median=0,   # uniform, or lognormal about the median
+        new_lo=1, new_hi=1,     # new tokens of a user, uniform
+        via="append",           # "write": "append" of new tokens behind the prefixes, or "restore" of prefixes in host chunks
+        rot_dim=0, pairs="halves",  # "rotate": rotated dims; (i, i + rot/2) or (2i, 2i + 1)
+        shape=1,
+    )
+    assert set(kw) <= set(c), kw
+    c.update(kw)
+    if name:
+        c["name"] = name
+    return c
+
+
+def listed():
+    return [
+        # One user's single new token: the smallest call of the smallest model, in fp32.
+        _case("decode_one", dtype="f32", kv_heads=4, head_dim=32, prefix_lo=256, prefix_hi=256, shape=31),
+        # One new token of each user of an ordinary batch, four query heads on a key head.
+        _case("decode_batch", kv_heads=8, group=4, users=64, prefix_median=1500, prefix_lo=128, prefix_hi=4096, shape=32),
+        # The same behind long histories: the time is that of reading the cache.
+        _case("decode_long", kv_heads=8, group=4, head_dim=128, users=32, prefix_lo=4096, prefix_hi=16384, shape=33),
+        # A few new interactions of each user behind long histories, a key head for every query head.
+        _case("extend_long", kv_heads=8, head_dim=128, users=32, prefix_lo=4096, prefix_hi=16384, new_lo=32, new_hi=32, shape=34),
+        # First visits: nothing cached, whole histories at once; the largest call.
+        _case("first_visits", kv_heads=8, group=2, head_dim=128, users=8, prefix_lo=0, prefix_hi=0, new_lo=4096, new_hi=4096, shape=35),
+        # fp32 rows, odd head counts, ragged new segments, some users without a history.
+        _case("ragged_f32", dtype="f32", kv_heads=5, group=3, head_dim=64, page=32, users=48, prefix_lo=0, prefix_hi=5000, new_lo=1, new_hi=37, shape=36),
+        # The write of a decode step: one row a user, single bytes of each group of tokens.
+        _case("append_decode", kind="write", kv_heads=8, group=4, head_dim=128, users=128, prefix_median=3000, prefix_lo=100, prefix_hi=12000, shape=37),
+        # Users whose history comes up from the host tier, quantised as it is written.
+        _case("restore_users", kind="write", via="restore", kv_heads=8, head_dim=128, page=32, users=24, prefix_lo=1000, prefix_hi=9000, shape=38),
+        # A user's history read back for the host tier.
+        _case("read_one", kind="read", kv_heads=4, head_dim=128, page=32, users=1, prefix_lo=6375, prefix_hi=6375, shape=39),
+        # Many users' histories read back, fp32 rows.
+        _case("read_users", kind="read", dtype="f32", kv_heads=8, head_dim=64, users=48, prefix_median=2500, prefix_lo=64, prefix_hi=8192, shape=40),
+        # Queries and keys of a decode step, half of the dims rotated.
+        _case("rotate_decode", kind="rotate", kv_heads=8, group=4, head_dim=128, rot_dim=64, users=64, prefix_median=1500, prefix_lo=128, prefix_hi=131072, shape=41),
+        # Queries and keys of whole histories, neighbours as pairs.
+        _case("rotate_visits", kind="rotate", kv_heads=8, group=2, head_dim=128, rot_dim=128, pairs="neighbours", users=12, prefix_lo=0, prefix_hi=500, new_lo=1500, new_hi=5000, shape=42),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    """One more case of the ranges above."""
+    kind = rng.choice(["attend", "attend", "attend", "write", "read", "rotate"])
+    for _ in range(500):
+        D = rng.choice([32, 64, 64, 128, 128])
+        c = dict(kind=kind, dtype=rng.choice(["bf16", "bf16", "f32"]), head_dim=D, page=rng.choice([16, 16, 32, 64]),
+                 kv_heads=rng.choice([1, 2, 3, 4, 5, 8, 16]), group=rng.choice([1, 1, 2, 3, 4, 5, 8]), users=_log_int(rng, 1, 192),
+                 shape=rng.randrange(1000, 1 << 20))
+        lo = _log_int(rng, 1, 12000)
+        c.update(prefix_lo=lo, prefix_hi=min(131072, int(lo * rng.uniform(1.0, 8.0))))
+        if rng.random() < 0.3:
+            c["prefix_median"] = int(math.sqrt(lo * c["prefix_hi"]))
+        hi = _log_int(rng, 1, 96)
+        if rng.random() < 0.25:
+            c.update(prefix_lo=0, prefix_hi=rng.choice([0, 300]), prefix_median=0, users=_log_int(rng, 1, 12))
+            hi = _log_int(rng, 96, 4096)
+        elif rng.random() < 0.4:
+            hi = 1
+        c.update(new_lo=max(1, hi // rng.choice([1, 2, 8])), new_hi=hi)
+        if kind == "write":
+            c["via"] = rng.choice(["append", "restore"])
+        if kind == "rotate":
+            c.update(rot_dim=8 * rng.randint(1, D // 8), pairs=rng.choice(["halves", "neighbours"]))
+        c = _case(**c)
+        prefix, new = _lengths(c)
+        Hq, t, n = c["kv_heads"] * c["group"], int((prefix + new).max()), int(new.max())
+        w = work(c)
+        if c["users"] * t * c["kv_heads"] * D <= 1.1e9 and w["bytes"] <= 1.6e9 and w["flops"] <= 5e11 and (
+                kind != "attend" or c["users"] * Hq * n * t <= 2.1e9):
+            if kind == "read" or c["via"] == "restore":
+                if prefix.max() < 1:
+                    continue
+            return c
+    raise RuntimeError("no case within the largest listed one's cost")
+
+
+def _lengths(case):
+    """(prefix lengths, new tokens) of the users, from the case alone."""
+    rng = np.random.default_rng([case["shape"], 6])
+    n, lo, hi = case["users"], case["prefix_lo"], case["prefix_hi"]
+    if case["prefix_median"]:
+        prefix = np.clip(np.rint(np.exp(rng.normal(np.log(case["prefix_median"]), 0.6, n))), lo, hi)
+    else:
+        prefix = rng.integers(lo, hi + 1, n)
+    return prefix.astype(np.int64), rng.integers(case["new_lo"], case["new_hi"] + 1, n).astype(np.int64)
+
+
+def _runs(case):
+    """Runs of tokens that a restore or a read-back moves: (user, first token, tokens)."""
+    prefix, _ = _lengths(case)
+    chunk = CHUNK if case["kind"] == "write" else 1 << 30
+    return [(u, s, min(chunk, int(p) - s)) for u, p in enumerate(prefix) for s in range(0, int(p), chunk)]
+
+
+def _granule(D):
+    return min(16, D // 4)
+
+
+def _views(pool, H, S, D):
+    """K codes [page, head, sub-block, dims / g, token, g], V codes [page, head, sub-block, dims / 4g, token / 4, dim, sixteen,
+    token], exponents [page, head, K or V, token] of the pool's bytes."""
+    g, n = _granule(D), S * D
+    return (pool[:, :, :n].unflatten(2, (S // 16, D // g, 16, g)), pool[:, :, n:2 * n].unflatten(2, (S // 16, D // (4 * g), 4, 16, g // 4, 4)),
+            pool[:, :, 2 * n:].unflatten(2, (2, S)))
+
+
+def _quantise(x):
+    """Codes (as bytes) and exponent bytes of rows [..., D]."""
+    x = x.float()
+    finite = torch.isfinite(x)
+    amax = torch.where(finite, x, 0.0).abs().amax(-1)
+    # the exponent field counts one up where the mantissa is above 1.75
+    e = ((amax.view(torch.int32) + 0x1FFFFF) >> 23) - 8
+    e = e.clamp(67, 187)
+    scale = ((254 - e) << 23).view(torch.float32)
+    y = (x * scale.unsqueeze(-1)).clamp(-448.0, 448.0)
+    y = torch.where(finite, y, math.nan)
+    return y.to(torch.float8_e4m3fn).view(torch.uint8), e.to(torch.uint8)
+
+
+def _values(codes, exps):
+    return codes.view(torch.float8_e4m3fn).float() * (exps.int() << 23).view(torch.float32).unsqueeze(-1)
+
+
+def _store(pool, S, page, slot, k, v):
+    """Rows k, v [N, H, D] quantised into the pool at (page, slot)."""
+    N, H, D = k.shape
+    g = _granule(D)
+    kc, vc, ex = _views(pool, H, S, D)
+    sub, t = slot // 16, slot % 16
+    codes, e = _quantise(k)
+    kc[page, :, sub, :, t, :] = codes.view(N, H, D // g, g)
+    ex[page, :, 0, slot] = e
+    codes, e = _quantise(v)
+    vc[page, :, sub, :, t // 4, :, :, t % 4] = codes.view(N, H, D // (4 * g), g // 4, 16).transpose(3, 4)
+    ex[page, :, 1, slot] = e
+
+
+def _load(pool, S, D, page, slot):
+    """K and V values at (page, slot), of any shape [...], as [..., H, D]."""
+    kc, vc, ex = _views(pool, pool.shape[1], S, D)
+    sub, t = slot // 16, slot % 16
+    k = _values(kc[page, :, sub, :, t, :].flatten(-2), ex[page, :, 0, slot])
+    v = _values(vc[page, :, sub, :, t // 4, :, :, t % 4].transpose(-1, -2).flatten(-3), ex[page, :, 1, slot])
+    return k, v
+
+
+def _dtype(case):
+    return torch.float32 if case["dtype"] == "f32" else torch.bfloat16
+
+
+def prepare(case, seed):
+    H, D, S, dt = case["kv_heads"], case["head_dim"], case["page"], _dtype(case)
+    Hq = H * case["group"]
+    prefix, new = _lengths(case)
+    rng = np.random.default_rng([seed, 9])
+    gen = torch.Generator(device=DEVICE)
+    gen.manual_seed(seed)
+
+    def ints(a, dtype=torch.int32):
+        return torch.from_numpy(np.ascontiguousarray(a)).to(DEVICE, dtype)
+
+    def rows(*shape):
+        """Rows of differing size, as projections give them."""
+        x = torch.empty(shape, device=DEVICE).normal_(generator=gen)
+        x *= torch.exp2(torch.empty(shape[:-1] + (1,), device=DEVICE).normal_(generator=gen) * 0.7)
+        return x.to(dt)
+
+    need = -(-(prefix + new) // S)
+    indptr = np.concatenate([[0], np.cumsum(need)])
+    pages = int(np.ceil(POOL_FACTOR * indptr[-1]))
+    N = int(new.sum())
+    st = dict(case=case, page_indptr=ints(indptr), page_indices=ints(rng.permutation(pages)[:indptr[-1]]), prefix_lens=ints(prefix),
+              new_indptr=ints(np.concatenate([[0], np.cumsum(new)])), total_new=N, max_new=int(new.max()),
+              max_total=int((prefix + new).max()), pages=pages, total_pages=int(indptr[-1]))
+    if case["kind"] == "rotate":
+        st["qkv"] = rows(N, Hq + 2 * H, D)                       # the projection's packed rows
+        st["weights"] = [(1.0 + 0.2 * torch.randn(D, device=DEVICE, generator=gen)).to(dt) for _ in range(2)]
+        r = case["rot_dim"]
+        st["freqs"] = torch.from_numpy(10000.0 ** (-np.arange(0, r, 2, dtype=np.float64) / r)).to(DEVICE)
+        st["out"] = [torch.empty(N, h, D, dtype=dt, device=DEVICE) for h in (Hq, H)]
+    else:
+        # the layer's pool, every slot written: 1.25 pages per held one
+        st["pool"] = torch.empty(pages, H, 2 * S * (D + 1), dtype=torch.uint8, device=DEVICE)
+        part = max(1, (1 << 27) // (H * S * D))
+        slot = torch.arange(S, device=DEVICE)
+        for p in range(0, pages, part):
+            page = torch.arange(p, min(pages, p + part), device=DEVICE).repeat_interleave(S)
+            n = len(page)
+            _store(st["pool"], S, page, slot.repeat(n // S), rows(n, H, D), rows(n, H, D))
+    if case["kind"] == "attend":
+        st["q"] = torch.empty(N, Hq, D, device=DEVICE).normal_(generator=gen).to(dt)
+        st["out"] = torch.empty(N, Hq, D, dtype=dt, device=DEVICE)
+    if case["kind"] in ("write", "read"):
+        runs = _runs(case) if case["kind"] == "read" or case["via"] == "restore" else list(zip(range(len(new)), prefix.tolist(), new.tolist()))
+        u, s, n = (np.asarray(a, np.int64) for a in zip(*runs))
+        st.update(num_segs=len(u), seg_user=ints(u), seg_pos=ints(s), seg_tok=ints(np.concatenate([[0], np.cumsum(n)]), torch.int64),
+                  max_seg=int(n.max()), tokens=int(n.sum()))
+        st["out"] = torch.empty(st["tokens"] * 2 * H * D, dtype=dt, device=DEVICE)
+        if case["kind"] == "write" and case["via"] == "append":
+            st["k"] = rows(N, H, D)
+            st["v"] = rows(N, Hq + 2 * H, D)[:, Hq + H:]         # where the packed projection left them
+        elif case["kind"] == "write":
+            st["staging"] = rows(2 * st["tokens"] * H, D).view(-1)
+    if own:
+        # the descriptors and the workspace that a program keeps between calls
+        import paper_2604_22881_amd as mts
+        st["mts"] = mts
+        st["meta"] = mts.BatchMeta(len(new), st["page_indptr"].data_ptr(), st["page_indices"].data_ptr(), st["prefix_lens"].data_ptr(),
+                                   st["new_indptr"].data_ptr(), N, st["max_new"], st["max_total"], st["total_pages"])
+        st["type"] = mts.MTS_F32 if dt == torch.float32 else mts.MTS_BF16
+        if "pool" in st:
+            st["desc"] = mts.CacheDesc(st["pool"].data_ptr(), -(-st["pool"].numel() // 256) * 256, mts.MTS_E4M3, 1, pages, S, H, D)
+        if case["kind"] == "attend":
+            st["ws_bytes"] = mts.mts_attn_q8_workspace_bytes(st["desc"], Hq, st["meta"])
+            st["ws"] = torch.empty(max(256, st["ws_bytes"]), dtype=torch.uint8, device=DEVICE)
+        if case["kind"] == "rotate":
+            st["desc"] = mts.QkDesc(st["type"], Hq, H, D, (Hq + 2 * H) * D, (Hq + 2 * H) * D, 0, 0, st["weights"][0].data_ptr(),
+                                    st["weights"][1].data_ptr(), 1, 1e-6, st["freqs"].data_ptr(), case["rot_dim"],
+                                    mts.MTS_ROPE_HALVES if case["pairs"] == "halves" else mts.MTS_ROPE_NEIGHBOURS)
+    return st
+
+
+def _row_places(st):
+    """(user, position) of the step's rows."""
+    new = st["new_indptr"].diff()
+    user = torch.repeat_interleave(new, output_size=st["total_new"])
+    pos = torch.arange(st["total_new"], device=DEVICE) - st["new_indptr"][user] + st["prefix_lens"][user]
+    return user, pos
+
+
+def _run_places(st):
+    """(user, position, run, token within the run) of the runs' tokens."""
+    seg = torch.repeat_interleave(st["seg_tok"].diff(), output_size=st["tokens"])
+    i = torch.arange(st["tokens"], device=DEVICE) - st["seg_tok"][seg]
+    return st["seg_user"][seg], st["seg_pos"][seg] + i, seg, i
+
+
+def _slots(st, user, pos):
+    S = st["case"]["page"]
+    return st["page_indices"][st["page_indptr"][user] + pos // S].long(), pos % S
+
+
+def _run_rows(st, seg, i):
+    """Where K and V of a run's token lie among the rows [2][n][...] of all runs."""
+    n = st["seg_tok"].diff()[seg]
+    k = 2 * st["seg_tok"][seg] + i
+    return k, k + n
+
+
+def _plain_read(st):
+    case = st["case"]
+    H, D, dt = case["kv_heads"], case["head_dim"], _dtype(case)
+    user, pos, seg, i = _run_places(st)
+    k, v = _load(st["pool"], case["page"], D, *_slots(st, user, pos))
+    at_k, at_v = _run_rows(st, seg, i)
+    out = torch.empty(2 * st["tokens"], H, D, dtype=dt, device=DEVICE)
+    out[at_k] = k.to(dt)
+    out[at_v] = v.to(dt)
+    return out.view(-1)
+
+
+def _plain_write(st):
+    case = st["case"]
+    H, D = case["kv_heads"], case["head_dim"]
+    if case["via"] == "append":
+        user, pos = _row_places(st)
+        k, v = st["k"], st["v"]
+    else:
+        user, pos, seg, i = _run_places(st)
+        at_k, at_v = _run_rows(st, seg, i)
+        rows = st["staging"].view(-1, H, D)
+        k, v = rows[at_k], rows[at_v]
+    _store(st["pool"], case["page"], *_slots(st, user, pos), k, v)
+    return _plain_read(st)
+
+
+def _plain_attend(st):
+    case = st["case"]
+    H, G, D, S = case["kv_heads"], case["group"], case["head_dim"], case["page"]
+    B, n, T = case["users"], st["max_new"], st["max_total"]
+    user, pos = _row_places(st)
+    i = pos - st["prefix_lens"][user]
+    q = torch.zeros(B, n, H, G, D, device=DEVICE)
+    q[user, i] = st["q"].view(-1, H, G, D).float()
+    j = torch.arange(T, device=DEVICE)
+    held = torch.minimum(st["page_indptr"][:-1, None] + j // S, st["page_indptr"][1:, None] - 1)
+    k, v = _load(st["pool"], S, D, st["page_indices"][held].long(), (j % S).expand(B, T))
+    s = q.permute(0, 2, 1, 3, 4).reshape(B, H, n * G, D) @ k.permute(0, 2, 3, 1)
+    s *= D ** -0.5
+    last = st["prefix_lens"][:, None] + torch.arange(n, device=DEVICE)           # a row's last visible key
+    hidden = (j > last.unsqueeze(-1)).repeat_interleave(G, 1).unsqueeze(1)
+    s.masked_fill_(hidden, -math.inf)
+    s -= s.amax(-1, keepdim=True)
+    s.exp_()
+    o = (s @ v.transpose(1, 2)) / s.sum(-1, keepdim=True)
+    o = o.view(B, H, n, G, D).permute(0, 2, 1, 3, 4)[user, i]
+    return o.reshape(-1, H * G, D).to(_dtype(case))
+
+
+def _plain_rotate(st):
+    case = st["case"]
+    H, D, r, dt = case["kv_heads"], case["head_dim"], case["rot_dim"], _dtype(case)
+    Hq = H * case["group"]
+    _, pos = _row_places(st)
+    angle = pos.double().unsqueeze(-1) * st["freqs"]             # far positions need 64 bits
+    cos, sin = angle.cos().float().unsqueeze(1), angle.sin().float().unsqueeze(1)
+
+    def one(x, w):
+        x = x.float()
+        x = x * torch.rsqrt(x.square().mean(-1, keepdim=True) + 1e-6) * w.float()
+        y = x[..., :r]
+        a, b = (y[..., :r // 2], y[..., r // 2:]) if case["pairs"] == "halves" else (y[..., ::2], y[..., 1::2])
+        a, b = a * cos - b * sin, b * cos + a * sin
+        y = torch.cat([a, b], -1) if case["pairs"] == "halves" else torch.stack([a, b], -1).flatten(-2)
+        return torch.cat([y, x[..., r:]], -1).to(dt)
+
+    return [one(st["qkv"][:, :Hq], st["weights"][0]), one(st["qkv"][:, Hq:Hq + H], st["weights"][1])]
+
+
+def run(st):
+    case = st["case"]
+    kind = case["kind"]
+    if not own:
+        return {"attend": _plain_attend, "write": _plain_write, "read": _plain_read, "rotate": _plain_rotate}[kind](st)
+    mts, desc, meta = st["mts"], st["desc"], st["meta"]
+    Hq = case["kv_heads"] * case["group"]
+    if kind == "attend":
+        mts.mts_attn_incremental_q8(desc, 0, st["type"], Hq, st["q"], st["out"], meta, 0.0, st["ws"], st["ws_bytes"])
+    elif kind == "rotate":
+        mts.mts_qk_norm_rope(desc, st["qkv"], st["qkv"][:, Hq:], st["out"][0], st["out"][1], meta)
+    else:
+        segs = (st["num_segs"], st["seg_user"], st["seg_pos"], st["seg_tok"], st["max_seg"])
+        if kind == "write" and case["via"] == "append":
+            mts.mts_kv_append_q8(desc, 0, st["type"], st["k"], st["v"], meta, 0, st["v"].stride(0))
+        elif kind == "write":
+            mts.mts_kv_unpack_q8(desc, 0, st["type"], st["staging"], *segs, meta)
+        mts.mts_kv_pack_q8(desc, 0, st["type"], st["out"], *segs, meta)
+    return st["out"]
+
+
+def work(case):
+    prefix, new = _lengths(case)
+    es, H, D = 4 if case["dtype"] == "f32" else 2, case["kv_heads"], case["head_dim"]
+    Hq, N = H * case["group"], int(new.sum())
+    stored, row = 2 * H * (D + 1), 2 * H * D * es                # a token's K and V in the pool, as rows
+    if case["kind"] == "attend":
+        pairs = int((new * prefix + new * (new + 1) // 2).sum())
+        return {"bytes": float(int((prefix + new).sum()) * stored + 2 * N * Hq * D * es), "flops": float(4 * D * Hq * pairs)}
+    if case["kind"] == "rotate":
+        return {"bytes": float(2 * N * (Hq + H) * D * es), "flops": float(10 * N * (Hq + H) * D)}
+    tokens = N if case["kind"] == "write" and case["via"] == "append" else int(prefix.sum())
+    passes = 2 if case["kind"] == "write" else 1
+    return {"bytes": float(passes * tokens * (stored + row)), "flops": float(passes * tokens * 4 * H * D)}
+
+
+# ---- the definitions in 64 bits -------------------------------------------------------------------
+
+def _code_values():
+    """The 256 values of e4m3: sign, four bits of exponent (bias 7), three of mantissa; the two all-ones codes are NaN."""
+    t = np.zeros(256)
+    for c in range(256):
+        e, m = (c >> 3) & 15, c & 7
+        t[c] = (-1.0 if c & 128 else 1.0) * (m / 8 * 2.0 ** -6 if e == 0 else (1 + m / 8) * 2.0 ** (e - 7))
+    t[[127, 255]] = np.nan
+    return torch.from_numpy(t).to(DEVICE)
+
+
+def _power(e):
+    """2^e in 64 bits, from its bit pattern (pow and exp2 may be off by a rounding)."""
+    return ((e.long() + 1023) << 52).view(torch.float64)
+
+
+def _stored_rows(st, user, tokens):
+    """[2][tokens][H][D] values of a user's tokens in 64 bits, every byte found by its offset."""
+    case = st["case"]
+    H, D, S = case["kv_heads"], case["head_dim"], case["page"]
+    g = min(16, D // 4)
+    pool = st["pool"].view(-1)
+    t = tokens.view(-1, 1, 1)
+    page = st["page_indices"].long()[int(st["page_indptr"][user]) + t // S]
+    h, d = torch.arange(H, device=DEVICE).view(1, -1, 1), torch.arange(D, device=DEVICE).view(1, 1, -1)
+    s, t16 = t % S, t % 16
+    base = (page * H + h) * (2 * S * (D + 1))
+    k = base + s // 16 * (16 * D) + (d // g * 16 + t16) * g + d % g
+    v = base + S * D + s // 16 * (16 * D) + (((d // (4 * g) * 4 + t16 // 4) * 16 + d % 16) * (g // 4) + d // 16 % (g // 4)) * 4 + t16 % 4
+    table = _code_values()
+    return torch.stack([table[pool[at].long()] * _power(pool[base + 2 * S * D + kv * S + s].int() - 127)
+                        for kv, at in enumerate((k, v))])
+
+
+def _rounded_rows(x):
+    """Rows [..., D] as the stored form keeps them, from its definition, in 64 bits."""
+    x = x.double()
+    m, e = torch.frexp(x.abs().amax(-1, keepdim=True))           # amax = m 2^e, m in [0.5, 1)
+    e = torch.where(m <= 0.875, e - 9, e - 8).clamp(-60, 60)     # 448 = 0.875 * 2^9
+    y = (x * _power(-e)).clamp(-448.0, 448.0)
+    step = _power(torch.frexp(y)[1].clamp(min=-5) - 4)
+    return torch.round(y / step) * step * _power(e)
+
+
+def exact(case, seed):
+    global own
+    was, own = own, False
+    st = prepare(case, seed)
+    own = was
+    H, G, D = case["kv_heads"], case["group"], case["head_dim"]
+    prefix, new = _lengths(case)
+    if case["kind"] == "attend":
+        out, at = [], 0
+        for u in range(case["users"]):
+            p, n = int(prefix[u]), int(new[u])
+            k, v = _stored_rows(st, u, torch.arange(p + n, device=DEVICE))
+            last = p + torch.arange(n, device=DEVICE).repeat_interleave(G)
+            bias = torch.where(torch.arange(p + n, device=DEVICE) > last.unsqueeze(-1), -math.inf, 0.0).double()
+            q = st["q"][at:at + n].double().view(n, H, G, D)
+            o = [torch.softmax((q[:, h].reshape(n * G, D) @ k[:, h].t().contiguous()) / math.sqrt(D) + bias, -1) @ v[:, h].contiguous()
+                 for h in range(H)]
+            out.append(torch.stack(o, 1).view(n, G, H, D).transpose(1, 2).reshape(n, H * G, D))
+            at += n
+        return torch.cat(out)
+    if case["kind"] == "rotate":
+        r, Hq = case["rot_dim"], H * G
+        pos = torch.from_numpy(np.concatenate([p + np.arange(n) for p, n in zip(prefix, new)]).astype(np.float64)).to(DEVICE)
+        turn = torch.polar(torch.ones(len(pos), r // 2, dtype=torch.float64, device=DEVICE), torch.outer(pos, st["freqs"])).unsqueeze(1)
+        res = []
+        for x, w in ((st["qkv"][:, :Hq], st["weights"][0]), (st["qkv"][:, Hq:Hq + H], st["weights"][1])):
+            x = x.double()
+            x = x / torch.sqrt((x * x).sum(-1, keepdim=True) / D + 1e-6) * w.double()
+            first = torch.arange(r // 2, device=DEVICE) * (1 if case["pairs"] == "halves" else 2)
+            second = first + (r // 2 if case["pairs"] == "halves" else 1)
+            z = torch.complex(x[..., first], x[..., second]) * turn
+            x[..., first], x[..., second] = z.real, z.imag
+            res.append(x)
+        return res
+    if case["kind"] == "read":
+        return torch.cat([_stored_rows(st, u, torch.arange(s, s + n, device=DEVICE)).view(-1) for u, s, n in _runs(case)])
+    if case["via"] == "restore":
+        return _rounded_rows(st["staging"].view(-1, D)).view(-1)
+    k, v = _rounded_rows(st["k"]), _rounded_rows(st["v"])
+    ends = np.concatenate([[0], np.cumsum(new)])
+    return torch.cat([x[a:b].reshape(-1) for a, b in zip(ends[:-1], ends[1:]) for x in (k, v)])
