@@ -3,8 +3,8 @@ at a time - norm and rotation of a step's queries and keys, the quantising write
 the attention that reads the stored form.
 
 Stored form: a row (one token, one head, K or V) of head_dim values is one exponent e and head_dim
-e4m3 codes; e is the smallest integer with amax <= 448 * 2^e over the row's finite values, held in
-[-60, 60], and a code is value * 2^-e rounded to nearest even.  A page is, head after head,
+e4m3 codes; e is the smallest integer with amax <= 464 * 2^e over the row's finite values (what rounds to
+the largest code, 448, or less), held in [-60, 60], and a code is value * 2^-e rounded to nearest even.  A page is, head after head,
 [K codes][V codes][K exponents + 127][V exponents + 127]; codes lie in sub-blocks of 16 tokens,
     K: [dims / g][16 tokens][g dims]              with g = min(16, head_dim / 4)
     V: [dims / 4g][4 groups of 4 tokens][16 dims][g / 4 sixteens of dims][4 tokens].
@@ -147,8 +147,8 @@ def _quantise(x):
     x = x.float()
     finite = torch.isfinite(x)
     amax = torch.where(finite, x, 0.0).abs().amax(-1)
-    # the exponent field counts one up where the mantissa is above 1.75
-    e = ((amax.view(torch.int32) + 0x1FFFFF) >> 23) - 8
+    # the exponent field counts one up where the mantissa is above 1.8125
+    e = ((amax.view(torch.int32) + 0x17FFFF) >> 23) - 8
     e = e.clamp(67, 187)
     scale = ((254 - e) << 23).view(torch.float32)
     y = (x * scale.unsqueeze(-1)).clamp(-448.0, 448.0)
@@ -431,7 +431,7 @@ def _rounded_rows(x):
     """Rows [..., D] as the stored form keeps them, from its definition, in 64 bits."""
     x = x.double()
     m, e = torch.frexp(x.abs().amax(-1, keepdim=True))           # amax = m 2^e, m in [0.5, 1)
-    e = torch.where(m <= 0.875, e - 9, e - 8).clamp(-60, 60)     # 448 = 0.875 * 2^9
+    e = torch.where(m <= 0.90625, e - 9, e - 8).clamp(-60, 60)   # 464 = 0.90625 * 2^9
     y = (x * _power(-e)).clamp(-448.0, 448.0)
     step = _power(torch.frexp(y)[1].clamp(min=-5) - 4)
     return torch.round(y / step) * step * _power(e)
