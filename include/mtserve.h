@@ -50,8 +50,8 @@
  *   [2 (K plane, V plane)][n][H][D], i.e. what is kept in host chunks and what the onload
  *   and offload buffers hold (Sec. 4.1 CPU tier, Sec. 4.2).
  *
- * Supported: dtype f32 or bf16; head_dim in {32, 64, 128}; page_size in {16, 32, 64};
- * any num_heads >= 1.
+ * Supported: dtype f32 or bf16, and e4m3 for the *_q8 calls, which have a layout of their own;
+ * head_dim in {32, 64, 128}; page_size in {16, 32, 64}; any num_heads >= 1.
  */
 #ifndef MTSERVE_H
 #define MTSERVE_H
@@ -72,17 +72,17 @@ enum {
   MTS_ERR_BUSY = -6         /* admission control refused the task (offload quota / buffer space); nothing was enqueued */
 };
 
-enum { MTS_F32 = 0, MTS_BF16 = 1 };
+enum { MTS_F32 = 0, MTS_BF16 = 1, MTS_E4M3 = 2 }; /* MTS_E4M3: pools of the *_q8 calls only */
 
 /* The paged pool (Sec. 4.1 "Paged Store").  Plain data, read during the call only. */
 typedef struct mts_cache_desc {
   void*   pool;               /* device, 256-byte aligned */
   int64_t layer_stride_bytes; /* >= num_pages * page_bytes, multiple of 256 */
-  int32_t dtype;              /* MTS_F32 or MTS_BF16 */
+  int32_t dtype;              /* MTS_F32 or MTS_BF16; MTS_E4M3 for the *_q8 calls */
   int32_t num_layers;
   int32_t num_pages;          /* pages per layer */
   int32_t page_size;          /* tokens per page, S */
-  int32_t num_heads;          /* H (queries, keys and values share it) */
+  int32_t num_heads;          /* H (queries, keys and values share it; of keys and values in the *_q8 calls) */
   int32_t head_dim;           /* D */
 } mts_cache_desc;
 
@@ -101,14 +101,16 @@ typedef struct mts_batch_meta {
   int32_t        total_pages;   /* = page_indptr[B] */
 } mts_batch_meta;
 
-/* Bytes of one page of one layer: 2 * H * S * D * es.  Returns < 0 on a bad descriptor. */
+/* Bytes of one page of one layer: 2 * H * S * D * es, of MTS_E4M3 2 * H * S * (D + 1).  Returns < 0 on a bad
+ * descriptor. */
 int64_t mts_page_bytes(const mts_cache_desc* cache);
 
 /* ceil(len / page_size): pages ONE user needs (rounding is per user, App. C.1). */
 int32_t mts_pages_for(int32_t len, int32_t page_size);
 
 /* Byte offset inside a page of element (kv: 0 = K, 1 = V; head; token slot in [0, S);
- * dim in [0, D)) under the layout stated above.  Host-only; < 0 on bad arguments. */
+ * dim in [0, D)) under the layout stated above (of MTS_E4M3: of its code, under the layout stated with
+ * the *_q8 calls).  Host-only; < 0 on bad arguments. */
 int64_t mts_elem_offset(const mts_cache_desc* cache, int32_t kv, int32_t head,
                         int32_t slot, int32_t dim);
 
@@ -320,6 +322,105 @@ int32_t mts_attn_incremental_staged(const mts_cache_desc* cache, int32_t layer, 
                                     int32_t chunk_tokens, void* out, const mts_batch_meta* meta,
                                     float sm_scale, void* workspace, int64_t workspace_bytes,
                                     void* stream);
+
+/*
+ * ---- 8-bit pool -----------------------------------------------------------------------------
+ * The same paged cache with half the bytes of bf16: mts_cache_desc with dtype MTS_E4M3, the same page
+ * tables and batch metadata.  The rows that are written and read (row_dtype, MTS_F32 or MTS_BF16)
+ * and the stored form differ, and query heads may share key heads.
+ *
+ * A row (one token, one head, K or V) of D values is stored as one exponent e and D codes of the
+ * 8-bit type e4m3 (finite values up to 448):  value = code * 2^e,  e = the smallest integer with
+ * max|x| <= 464 * 2^e over the row's finite values (what still rounds to 448), held in [-60, 60], and
+ * code = x * 2^-e rounded to nearest even, magnitudes above 448 to 448.  An infinity or NaN is stored as NaN.
+ * A stored value is off by at most half a step of three mantissa bits (2^-4 of it) or 2^(e-10); magnitudes above
+ * 448 * 2^60 are stored as that, those up to 2^-70 as 0.
+ * Every stored value is a bf16 value, and storing a row that was read back gives the same bytes.
+ *
+ * Layout: layer, page and head as above, with a head's block of a page
+ *   [K codes, S*D][V codes, S*D][K: e + 127, S][V: e + 127, S] bytes,  2*S*(D+1) in all;
+ *   codes in sub-blocks of 16 tokens, 16*D bytes each; with g = min(16, D/4), token t, dim d,
+ *   K:  (d/g * 16 + t) * g + d % g
+ *   V:  (((d/(4g) * 4 + t/4) * 16 + d % 16) * (g/4) + (d/16) % (g/4)) * 4 + t % 4.
+ * mts_elem_offset() evaluates this map, mts_q8_exp_offset() that of the exponents.
+ */
+/* Byte offset inside a page of the exponent byte of row (kv, head, token slot).  Host-only; < 0 on bad arguments. */
+int64_t mts_q8_exp_offset(const mts_cache_desc* cache, int32_t kv, int32_t head, int32_t slot);
+
+/*
+ * mts_kv_append into an 8-bit pool: the step's rows are quantised as they are written.  The rows of a
+ * token's H heads are contiguous; from one token to the next lie k_token_stride / v_token_stride
+ * elements (0: H*D; a multiple of 16 bytes, at least H*D), so that rows can be taken from where a
+ * packed projection left them.  Tokens of other calls that share a sub-block stay as they are.
+ */
+int32_t mts_kv_append_q8(const mts_cache_desc* cache, int32_t layer, int32_t row_dtype, const void* k_new,
+                         int64_t k_token_stride, const void* v_new, int64_t v_token_stride,
+                         const mts_batch_meta* meta, void* stream);
+/* mts_kv_unpack and mts_kv_pack of an 8-bit pool: runs of rows [2][n][H][D] of row_dtype are quantised as they
+ * are written, and read back as the values that their codes stand for (exact in either type). */
+int32_t mts_kv_unpack_q8(const mts_cache_desc* cache, int32_t layer, int32_t row_dtype, const void* staging,
+                         int32_t num_segs, const int32_t* seg_user, const int32_t* seg_pos,
+                         const int64_t* seg_tok_indptr, int32_t max_seg_tokens, const mts_batch_meta* meta,
+                         void* stream);
+int32_t mts_kv_pack_q8(const mts_cache_desc* cache, int32_t layer, int32_t row_dtype, void* staging_out,
+                       int32_t num_segs, const int32_t* seg_user, const int32_t* seg_pos,
+                       const int64_t* seg_tok_indptr, int32_t max_seg_tokens, const mts_batch_meta* meta,
+                       void* stream);
+
+/*
+ * mts_attn_incremental over an 8-bit pool, with num_q_heads query heads, a multiple G of the pool's H key
+ * heads: query head h reads key head h / G (G = 1: a key head each; H = 1: one for all).  q and out are
+ * device [total_new][num_q_heads][D] of row_dtype, 16-byte aligned.  Any segment lengths, from one new token
+ * behind a long history (the keys are cut into stretches that are joined by a second kernel) to a whole
+ * history at once.  The result is that of the stored values: logits from exact products with fp32 sums,
+ * fp32 softmax statistics and accumulators.  bf16 rows: weights take part in the weighted sum of V rounded to
+ * fp16 (half a step: 2^-12 of the weight); fp32 rows: queries with 24 bits, weights with 22.  A weight times its row's
+ * 2^e below 2^-34 of the largest such product so far may count as 0 in the weighted sum.  Keys behind a query do not reach
+ * its output, whatever they hold.
+ * The workspace is as for mts_attn_incremental; a call given less than mts_attn_q8_workspace_bytes is
+ * refused with MTS_ERR_WORKSPACE.  max_total_len <= 2^30; mts_attn_set_tuning has no bearing on this call.
+ */
+int64_t mts_attn_q8_workspace_bytes(const mts_cache_desc* cache, int32_t num_q_heads, const mts_batch_meta* meta);
+int32_t mts_attn_incremental_q8(const mts_cache_desc* cache, int32_t layer, int32_t row_dtype, int32_t num_q_heads,
+                                const void* q, void* out, const mts_batch_meta* meta, float sm_scale,
+                                void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * ---- Norm and rotation of a step's queries and keys -----------------------------------------
+ * What stands between a layer's projection and its append and attention, for either pool, in one
+ * pass.  For every token of the step (row r of user u, at position p = prefix_lens[u] + r - new_indptr[u])
+ * and each of its query and key heads:
+ *   norm      y = x / sqrt(mean(x^2) + eps) * w   (MTS_NORM_RMS), or y = x * w  (MTS_NORM_NONE); w NULL: ones
+ *   rotation  of rot_dim / 2 pairs by t_i = p * freqs[i]:  (a, b) -> (a cos t - b sin t, b cos t + a sin t)
+ *             pair i is dims (i, i + rot_dim/2) (MTS_ROPE_HALVES) or (2i, 2i + 1) (MTS_ROPE_NEIGHBOURS);
+ *             dims from rot_dim on are not rotated.  t_i is computed in 64 bits.
+ * Computed in fp32 and rounded to the type once.  Reads meta's prefix_lens, new_indptr and scalars only.
+ * A token's heads are contiguous rows of head_dim; from one token to the next lie *_token_stride elements
+ * (0: heads * head_dim; a multiple of 16 bytes, at least that).  An output may be its own input (same address,
+ * same stride), but may not overlap the inputs otherwise.
+ */
+enum { MTS_NORM_NONE = 0, MTS_NORM_RMS = 1 };
+enum { MTS_ROPE_HALVES = 0, MTS_ROPE_NEIGHBOURS = 1 };
+typedef struct mts_qk_desc {
+  int32_t       dtype;              /* of rows and weights: MTS_F32 or MTS_BF16 */
+  int32_t       num_q_heads;
+  int32_t       num_k_heads;
+  int32_t       head_dim;           /* 32, 64 or 128 */
+  int64_t       q_token_stride;     /* elements, see above */
+  int64_t       k_token_stride;
+  int64_t       q_out_token_stride;
+  int64_t       k_out_token_stride;
+  const void*   q_weight;           /* device [head_dim], 16-byte aligned, or NULL */
+  const void*   k_weight;
+  int32_t       norm;               /* MTS_NORM_* */
+  float         eps;                /* >= 0, for MTS_NORM_RMS */
+  const double* freqs;              /* device [rot_dim / 2], radians per position */
+  int32_t       rot_dim;            /* multiple of 8 in [0, head_dim]; 0: no rotation */
+  int32_t       pairs;              /* MTS_ROPE_* */
+} mts_qk_desc;
+/* q, k: device, 16-byte aligned, as are q_out, k_out. */
+int32_t mts_qk_norm_rope(const mts_qk_desc* desc, const void* q, const void* k, void* q_out, void* k_out,
+                         const mts_batch_meta* meta, void* stream);
 
 /* Host<->device staging copies on `stream` (hipMemcpyAsync); `host` should be pinned for the
  * copy to be asynchronous (Sec. 4.2, DMA between pinned buffers and the onload / offload buffers). */

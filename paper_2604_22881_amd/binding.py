@@ -16,7 +16,9 @@ LIB_PATH = os.path.join(PKG_DIR, "libmtserve_hip.so")
 
 MTS_OK, MTS_ERR_INVALID_ARG, MTS_ERR_UNSUPPORTED, MTS_ERR_SHAPE, MTS_ERR_WORKSPACE, MTS_ERR_HIP = 0, -1, -2, -3, -4, -5
 MTS_ERR_BUSY = -6
-MTS_F32, MTS_BF16 = 0, 1
+MTS_F32, MTS_BF16, MTS_E4M3 = 0, 1, 2
+MTS_NORM_NONE, MTS_NORM_RMS = 0, 1
+MTS_ROPE_HALVES, MTS_ROPE_NEIGHBOURS = 0, 1
 
 EXPORTS = (
     "mts_page_bytes", "mts_pages_for", "mts_elem_offset", "mts_kv_unpack", "mts_kv_pack",
@@ -24,6 +26,8 @@ EXPORTS = (
     "mts_kv_append", "mts_attn_workspace_bytes", "mts_attn_set_tuning", "mts_attn_incremental", "mts_attn_incremental_noalloc", "mts_attn_pointwise",
     "mts_attn_unappended_appends", "mts_attn_incremental_unappended", "mts_attn_pointwise_unappended",
     "mts_attn_incremental_staged",
+    "mts_q8_exp_offset", "mts_kv_append_q8", "mts_kv_unpack_q8", "mts_kv_pack_q8", "mts_attn_q8_workspace_bytes", "mts_attn_incremental_q8",
+    "mts_qk_norm_rope",
     "mts_stage_h2d_async", "mts_stage_d2h_async", "mts_diag_stream_read", "mts_last_error", "mts_version",
     "mts_xfer_create", "mts_xfer_destroy", "mts_xfer_onload_submit", "mts_xfer_onload_wait_layer",
     "mts_xfer_offload_submit", "mts_xfer_offload_pending_tokens", "mts_xfer_drain",
@@ -48,6 +52,13 @@ class BatchMeta(C.Structure):
     _fields_ = [("batch", C.c_int32), ("page_indptr", C.c_void_p), ("page_indices", C.c_void_p),
                 ("prefix_lens", C.c_void_p), ("new_indptr", C.c_void_p), ("total_new", C.c_int32),
                 ("max_new", C.c_int32), ("max_total_len", C.c_int32), ("total_pages", C.c_int32)]
+
+
+class QkDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("num_q_heads", C.c_int32), ("num_k_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("q_token_stride", C.c_int64), ("k_token_stride", C.c_int64), ("q_out_token_stride", C.c_int64),
+                ("k_out_token_stride", C.c_int64), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("norm", C.c_int32),
+                ("eps", C.c_float), ("freqs", C.c_void_p), ("rot_dim", C.c_int32), ("pairs", C.c_int32)]
 
 
 class AttnTuning(C.Structure):
@@ -107,6 +118,13 @@ def lib():
         "mts_attn_incremental_unappended": (I32, [DESC, I32, P, P, P, P, META, F32, P, I64, P]),
         "mts_attn_pointwise_unappended": (I32, [DESC, I32, P, P, P, P, META, F32, F32, P, I64, P]),
         "mts_attn_incremental_staged": (I32, [DESC, I32, P, P, P, P, P, P, I32, P, META, F32, P, I64, P]),
+        "mts_q8_exp_offset": (I64, [DESC, I32, I32, I32]),
+        "mts_kv_append_q8": (I32, [DESC, I32, I32, P, I64, P, I64, META, P]),
+        "mts_kv_unpack_q8": (I32, [DESC, I32, I32, P, I32, P, P, P, I32, META, P]),
+        "mts_kv_pack_q8": (I32, [DESC, I32, I32, P, I32, P, P, P, I32, META, P]),
+        "mts_attn_q8_workspace_bytes": (I64, [DESC, I32, META]),
+        "mts_attn_incremental_q8": (I32, [DESC, I32, I32, I32, P, P, META, F32, P, I64, P]),
+        "mts_qk_norm_rope": (I32, [C.POINTER(QkDesc), P, P, P, P, META, P]),
         "mts_stage_h2d_async": (I32, [P, P, I64, P]),
         "mts_stage_d2h_async": (I32, [P, P, I64, P]),
         "mts_diag_stream_read": (I32, [P, I64, P, P]),
@@ -300,6 +318,43 @@ def mts_attn_incremental_staged(desc, layer, q, k_new, v_new, staged_rows, stage
                                                     int(chunk_tokens), _ptr(out), meta, float(sm_scale),
                                                     None if workspace is None else _ptr(workspace),
                                                     int(workspace_bytes), _stream(stream)))
+
+
+# ---- 8-bit pool -----------------------------------------------------------------------------
+def mts_q8_exp_offset(desc: CacheDesc, kv, head, slot):
+    return _check(lib().mts_q8_exp_offset(desc, kv, head, slot))
+
+
+def mts_kv_append_q8(desc, layer, row_dtype, k_new, v_new, meta, k_token_stride=0, v_token_stride=0, stream=None):
+    return _check(lib().mts_kv_append_q8(desc, layer, row_dtype, _ptr(k_new), k_token_stride, _ptr(v_new), v_token_stride,
+                                         meta, _stream(stream)))
+
+
+def mts_kv_unpack_q8(desc, layer, row_dtype, staging, num_segs, seg_user, seg_pos, seg_tok_indptr, max_seg_tokens,
+                     meta, stream=None):
+    return _check(lib().mts_kv_unpack_q8(desc, layer, row_dtype, _ptr(staging), num_segs, _ptr(seg_user), _ptr(seg_pos),
+                                         _ptr(seg_tok_indptr), max_seg_tokens, meta, _stream(stream)))
+
+
+def mts_kv_pack_q8(desc, layer, row_dtype, staging_out, num_segs, seg_user, seg_pos, seg_tok_indptr, max_seg_tokens,
+                   meta, stream=None):
+    return _check(lib().mts_kv_pack_q8(desc, layer, row_dtype, _ptr(staging_out), num_segs, _ptr(seg_user), _ptr(seg_pos),
+                                       _ptr(seg_tok_indptr), max_seg_tokens, meta, _stream(stream)))
+
+
+def mts_attn_q8_workspace_bytes(desc: CacheDesc, num_q_heads, meta: BatchMeta):
+    return _check(lib().mts_attn_q8_workspace_bytes(desc, num_q_heads, meta))
+
+
+def mts_attn_incremental_q8(desc, layer, row_dtype, num_q_heads, q, out, meta, sm_scale=0.0, workspace=None, workspace_bytes=0,
+                            stream=None):
+    return _check(lib().mts_attn_incremental_q8(desc, layer, row_dtype, num_q_heads, _ptr(q), _ptr(out), meta, float(sm_scale),
+                                                None if workspace is None else _ptr(workspace), int(workspace_bytes),
+                                                _stream(stream)))
+
+
+def mts_qk_norm_rope(desc: QkDesc, q, k, q_out, k_out, meta, stream=None):
+    return _check(lib().mts_qk_norm_rope(desc, _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), meta, _stream(stream)))
 
 
 # ---- transfer pipeline --------------------------------------------------------------------

@@ -11,6 +11,7 @@
 #include "../../include/mtserve.h"
 #include "mts_attn_rules.hpp"
 #include "mts_internal.hpp"
+#include "mts_q8.hpp"
 
 namespace {
 
@@ -28,11 +29,8 @@ bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p
 
 int elem_bytes(int32_t dtype) { return dtype == MTS_F32 ? 4 : (dtype == MTS_BF16 ? 2 : 0); }
 
-// Validates the descriptor (and the layer, unless layer < -1 is passed as "not needed").
-int32_t check_cache(const mts_cache_desc* c, int32_t layer, bool need_pool, mts::PoolGeom* g) {
-  if (!c) return fail(MTS_ERR_INVALID_ARG, "cache descriptor is NULL");
-  const int es = elem_bytes(c->dtype);
-  if (!es) return fail(MTS_ERR_UNSUPPORTED, "dtype %d is neither MTS_F32 nor MTS_BF16", c->dtype);
+// What holds for a pool of any element type.
+int32_t check_shape(const mts_cache_desc* c) {
   if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128)
     return fail(MTS_ERR_UNSUPPORTED, "head_dim %d not in {32, 64, 128}", c->head_dim);
   if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64)
@@ -41,18 +39,31 @@ int32_t check_cache(const mts_cache_desc* c, int32_t layer, bool need_pool, mts:
     return fail(MTS_ERR_INVALID_ARG, "num_heads %d out of range [1, 65535]", c->num_heads);
   if (c->num_layers < 1 || c->num_pages < 1)
     return fail(MTS_ERR_INVALID_ARG, "num_layers %d and num_pages %d must be >= 1", c->num_layers, c->num_pages);
+  return MTS_OK;
+}
+
+int32_t check_pool(const mts_cache_desc* c, int32_t layer, int64_t page_bytes) {
+  if (!c->pool) return fail(MTS_ERR_INVALID_ARG, "pool is NULL");
+  if (!aligned(c->pool, 256)) return fail(MTS_ERR_INVALID_ARG, "pool is not 256-byte aligned");
+  if (c->layer_stride_bytes < page_bytes * c->num_pages)
+    return fail(MTS_ERR_SHAPE, "layer_stride_bytes %lld < num_pages * page_bytes %lld",
+                (long long)c->layer_stride_bytes, (long long)(page_bytes * c->num_pages));
+  if (c->layer_stride_bytes % 256)
+    return fail(MTS_ERR_INVALID_ARG, "layer_stride_bytes is not a multiple of 256");
+  if (layer < 0 || layer >= c->num_layers)
+    return fail(MTS_ERR_INVALID_ARG, "layer %d out of range [0, %d)", layer, c->num_layers);
+  return MTS_OK;
+}
+
+// Validates the descriptor, and with need_pool the pool and the layer.
+int32_t check_cache(const mts_cache_desc* c, int32_t layer, bool need_pool, mts::PoolGeom* g) {
+  if (!c) return fail(MTS_ERR_INVALID_ARG, "cache descriptor is NULL");
+  const int es = elem_bytes(c->dtype);
+  if (!es) return fail(MTS_ERR_UNSUPPORTED, "dtype %d is neither MTS_F32 nor MTS_BF16", c->dtype);
+  int32_t st;
+  if ((st = check_shape(c)) != MTS_OK) return st;
   const int64_t page_bytes = 2ll * c->num_heads * c->page_size * c->head_dim * es;
-  if (need_pool) {
-    if (!c->pool) return fail(MTS_ERR_INVALID_ARG, "pool is NULL");
-    if (!aligned(c->pool, 256)) return fail(MTS_ERR_INVALID_ARG, "pool is not 256-byte aligned");
-    if (c->layer_stride_bytes < page_bytes * c->num_pages)
-      return fail(MTS_ERR_SHAPE, "layer_stride_bytes %lld < num_pages * page_bytes %lld",
-                  (long long)c->layer_stride_bytes, (long long)(page_bytes * c->num_pages));
-    if (c->layer_stride_bytes % 256)
-      return fail(MTS_ERR_INVALID_ARG, "layer_stride_bytes is not a multiple of 256");
-    if (layer < 0 || layer >= c->num_layers)
-      return fail(MTS_ERR_INVALID_ARG, "layer %d out of range [0, %d)", layer, c->num_layers);
-  }
+  if (need_pool && (st = check_pool(c, layer, page_bytes)) != MTS_OK) return st;
   if (g) {
     g->layer_base = need_pool ? static_cast<char*>(c->pool) + (int64_t)layer * c->layer_stride_bytes : nullptr;
     g->page_bytes = page_bytes;
@@ -63,6 +74,40 @@ int32_t check_cache(const mts_cache_desc* c, int32_t layer, bool need_pool, mts:
     g->es = es;
     g->sub_shift = c->page_size == 16 ? 0 : (c->page_size == 32 ? 1 : 2);
   }
+  return MTS_OK;
+}
+
+// The same for a pool of MTS_E4M3.
+int32_t check_q8_cache(const mts_cache_desc* c, int32_t layer, bool need_pool, mts::Q8Geom* g) {
+  if (!c) return fail(MTS_ERR_INVALID_ARG, "cache descriptor is NULL");
+  if (c->dtype != MTS_E4M3) return fail(MTS_ERR_UNSUPPORTED, "dtype %d of the pool is not MTS_E4M3", c->dtype);
+  int32_t st;
+  if ((st = check_shape(c)) != MTS_OK) return st;
+  const int64_t page_bytes = c->num_heads * mts::q8_head_bytes(c->page_size, c->head_dim);
+  if (need_pool && (st = check_pool(c, layer, page_bytes)) != MTS_OK) return st;
+  g->layer_base = need_pool ? static_cast<char*>(c->pool) + (int64_t)layer * c->layer_stride_bytes : nullptr;
+  g->page_bytes = page_bytes;
+  g->num_pages = c->num_pages;
+  g->S = c->page_size;
+  g->H = c->num_heads;
+  g->D = c->head_dim;
+  g->sub_shift = c->page_size == 16 ? 0 : (c->page_size == 32 ? 1 : 2);
+  return MTS_OK;
+}
+
+int32_t check_row_type(int32_t dtype) {
+  if (!elem_bytes(dtype)) return fail(MTS_ERR_UNSUPPORTED, "row dtype %d is neither MTS_F32 nor MTS_BF16", dtype);
+  return MTS_OK;
+}
+
+// Bytes from a token's rows to the next one's; 0 elements: the rows of `heads` heads follow one another.
+int32_t row_stride(const char* name, int64_t elements, int32_t heads, int32_t head_dim, int es, int64_t* bytes) {
+  const int64_t row = (int64_t)heads * head_dim;
+  if (elements == 0) elements = row;
+  if (elements < row || elements > (1ll << 40))
+    return fail(MTS_ERR_SHAPE, "%s %lld is not 0 and less than a token's %lld elements (or above 2^40)", name, (long long)elements, (long long)row);
+  if (elements * es % 16) return fail(MTS_ERR_INVALID_ARG, "%s is not a multiple of 16 bytes", name);
+  *bytes = elements * es;
   return MTS_OK;
 }
 
@@ -322,9 +367,14 @@ extern "C" {
 
 const char* mts_last_error(void) { return g_err; }
 
-int32_t mts_version(void) { return 100; }
+int32_t mts_version(void) { return 200; }
 
 int64_t mts_page_bytes(const mts_cache_desc* cache) {
+  if (cache && cache->dtype == MTS_E4M3) {
+    mts::Q8Geom q{};
+    const int32_t st = check_q8_cache(cache, 0, false, &q);
+    return st != MTS_OK ? st : q.page_bytes;
+  }
   mts::PoolGeom g{};
   const int32_t st = check_cache(cache, 0, false, &g);
   return st != MTS_OK ? st : g.page_bytes;
@@ -336,12 +386,23 @@ int32_t mts_pages_for(int32_t len, int32_t page_size) {
 }
 
 int64_t mts_elem_offset(const mts_cache_desc* cache, int32_t kv, int32_t head, int32_t slot, int32_t dim) {
+  const bool q8 = cache && cache->dtype == MTS_E4M3;
   mts::PoolGeom g{};
-  const int32_t st = check_cache(cache, 0, false, &g);
+  mts::Q8Geom q{};
+  const int32_t st = q8 ? check_q8_cache(cache, 0, false, &q) : check_cache(cache, 0, false, &g);
   if (st != MTS_OK) return st;
-  if (kv < 0 || kv > 1 || head < 0 || head >= g.H || slot < 0 || slot >= g.S || dim < 0 || dim >= g.D)
+  if (kv < 0 || kv > 1 || head < 0 || head >= cache->num_heads || slot < 0 || slot >= cache->page_size || dim < 0 || dim >= cache->head_dim)
     return fail(MTS_ERR_INVALID_ARG, "element (kv %d, head %d, slot %d, dim %d) out of range", kv, head, slot, dim);
-  return mts::elem_offset(kv, head, slot, dim, g.S, g.D, g.es);
+  return q8 ? mts::q8_code_offset(kv, head, slot, dim, q.S, q.D) : mts::elem_offset(kv, head, slot, dim, g.S, g.D, g.es);
+}
+
+int64_t mts_q8_exp_offset(const mts_cache_desc* cache, int32_t kv, int32_t head, int32_t slot) {
+  mts::Q8Geom g{};
+  const int32_t st = check_q8_cache(cache, 0, false, &g);
+  if (st != MTS_OK) return st;
+  if (kv < 0 || kv > 1 || head < 0 || head >= g.H || slot < 0 || slot >= g.S)
+    return fail(MTS_ERR_INVALID_ARG, "row (kv %d, head %d, slot %d) out of range", kv, head, slot);
+  return mts::q8_exp_offset(kv, head, slot, g.S, g.D);
 }
 
 int32_t mts_kv_unpack(const mts_cache_desc* cache, int32_t layer, const void* staging, int32_t num_segs,
@@ -635,6 +696,155 @@ int32_t mts_attn_incremental_staged(const mts_cache_desc* cache, int32_t layer, 
   const mts::StagedHistories hist{staged_rows, staged_first_run, staged_run_tok, chunk_tokens};
   return attention_call("mts_attn_incremental_staged launch", cache, layer, q, out, meta, sm_scale, 0.f, workspace,
                         workspace_bytes, stream, true, k_new, v_new, &hist);
+}
+
+// ---- 8-bit pool ----------------------------------------------------------------------------------
+
+int32_t mts_kv_append_q8(const mts_cache_desc* cache, int32_t layer, int32_t row_dtype, const void* k_new, int64_t k_token_stride,
+                         const void* v_new, int64_t v_token_stride, const mts_batch_meta* meta, void* stream) {
+  mts::Q8Geom g{};
+  mts::BatchDev b{};
+  int32_t st;
+  if ((st = check_q8_cache(cache, layer, true, &g)) != MTS_OK) return st;
+  if ((st = check_row_type(row_dtype)) != MTS_OK) return st;
+  if ((st = check_meta(meta, true, true, &b)) != MTS_OK) return st;
+  int64_t ks = 0, vs = 0;
+  if ((st = row_stride("k_token_stride", k_token_stride, g.H, g.D, elem_bytes(row_dtype), &ks)) != MTS_OK) return st;
+  if ((st = row_stride("v_token_stride", v_token_stride, g.H, g.D, elem_bytes(row_dtype), &vs)) != MTS_OK) return st;
+  if (b.batch == 0 || b.total_new == 0) return MTS_OK;
+  if (!k_new || !v_new) return fail(MTS_ERR_INVALID_ARG, "k_new / v_new is NULL");
+  if (!aligned(k_new, 16) || !aligned(v_new, 16))
+    return fail(MTS_ERR_INVALID_ARG, "k_new / v_new is not 16-byte aligned");
+  return hip_status(mts::launch_q8_append(g, row_dtype == MTS_F32, k_new, ks, v_new, vs, b, static_cast<hipStream_t>(stream)),
+                    "mts_kv_append_q8 launch");
+}
+
+// mts_kv_unpack_q8 / mts_kv_pack_q8
+static int32_t move_q8(bool pack, const mts_cache_desc* cache, int32_t layer, int32_t row_dtype, void* staging, int32_t num_segs,
+                       const int32_t* seg_user, const int32_t* seg_pos, const int64_t* seg_tok_indptr, int32_t max_seg_tokens,
+                       const mts_batch_meta* meta, void* stream) {
+  mts::Q8Geom g{};
+  mts::BatchDev b{};
+  mts::SegDev s{};
+  int32_t st;
+  if ((st = check_q8_cache(cache, layer, true, &g)) != MTS_OK) return st;
+  if ((st = check_row_type(row_dtype)) != MTS_OK) return st;
+  if ((st = check_meta(meta, false, true, &b)) != MTS_OK) return st;
+  if ((st = check_segs(num_segs, seg_user, seg_pos, seg_tok_indptr, max_seg_tokens, &s)) != MTS_OK) return st;
+  if (num_segs == 0 || max_seg_tokens == 0) return MTS_OK;
+  const char* name = pack ? "staging_out" : "staging";
+  if (!staging) return fail(MTS_ERR_INVALID_ARG, "%s is NULL", name);
+  if (!aligned(staging, 16)) return fail(MTS_ERR_INVALID_ARG, "%s is not 16-byte aligned", name);
+  if (b.batch == 0) return fail(MTS_ERR_SHAPE, "segments given for an empty batch");
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  return hip_status(pack ? mts::launch_q8_pack(g, row_dtype == MTS_F32, staging, s, b, hs)
+                         : mts::launch_q8_unpack(g, row_dtype == MTS_F32, staging, s, b, hs),
+                    pack ? "mts_kv_pack_q8 launch" : "mts_kv_unpack_q8 launch");
+}
+
+int32_t mts_kv_unpack_q8(const mts_cache_desc* cache, int32_t layer, int32_t row_dtype, const void* staging, int32_t num_segs,
+                         const int32_t* seg_user, const int32_t* seg_pos, const int64_t* seg_tok_indptr, int32_t max_seg_tokens,
+                         const mts_batch_meta* meta, void* stream) {
+  return move_q8(false, cache, layer, row_dtype, const_cast<void*>(staging), num_segs, seg_user, seg_pos, seg_tok_indptr,
+                 max_seg_tokens, meta, stream);
+}
+
+int32_t mts_kv_pack_q8(const mts_cache_desc* cache, int32_t layer, int32_t row_dtype, void* staging_out, int32_t num_segs,
+                       const int32_t* seg_user, const int32_t* seg_pos, const int64_t* seg_tok_indptr, int32_t max_seg_tokens,
+                       const mts_batch_meta* meta, void* stream) {
+  return move_q8(true, cache, layer, row_dtype, staging_out, num_segs, seg_user, seg_pos, seg_tok_indptr, max_seg_tokens, meta, stream);
+}
+
+static int32_t check_q_heads(const mts::Q8Geom& g, int32_t num_q_heads) {
+  if (num_q_heads < 1 || num_q_heads > 65535) return fail(MTS_ERR_INVALID_ARG, "num_q_heads %d out of range [1, 65535]", num_q_heads);
+  if (num_q_heads % g.H) return fail(MTS_ERR_SHAPE, "num_q_heads %d is not a multiple of num_heads %d", num_q_heads, g.H);
+  return MTS_OK;
+}
+
+static int32_t too_large_q8(const mts::BatchDev& b) {
+  return fail(MTS_ERR_UNSUPPORTED, "batch %d x max_new %d query rows make more tiles than one call holds (2^31), or max_total_len %d "
+              "exceeds 2^30", b.batch, b.max_new, b.max_total_len);
+}
+
+int64_t mts_attn_q8_workspace_bytes(const mts_cache_desc* cache, int32_t num_q_heads, const mts_batch_meta* meta) {
+  mts::Q8Geom g{};
+  mts::BatchDev b{};
+  int32_t st;
+  if ((st = check_q8_cache(cache, 0, false, &g)) != MTS_OK) return st;
+  if ((st = check_q_heads(g, num_q_heads)) != MTS_OK) return st;
+  if ((st = check_meta(meta, true, false, &b)) != MTS_OK) return st;
+  const mts::Q8AttnPlan p = mts::plan_q8_attention(g, num_q_heads, b);
+  if (p.too_large) return too_large_q8(b);
+  return p.ws_bytes;
+}
+
+int32_t mts_attn_incremental_q8(const mts_cache_desc* cache, int32_t layer, int32_t row_dtype, int32_t num_q_heads, const void* q,
+                                void* out, const mts_batch_meta* meta, float sm_scale, void* workspace, int64_t workspace_bytes,
+                                void* stream) {
+  mts::Q8Geom g{};
+  mts::BatchDev b{};
+  int32_t st;
+  if ((st = check_q8_cache(cache, layer, true, &g)) != MTS_OK) return st;
+  if ((st = check_row_type(row_dtype)) != MTS_OK) return st;
+  if ((st = check_q_heads(g, num_q_heads)) != MTS_OK) return st;
+  if ((st = check_meta(meta, true, true, &b)) != MTS_OK) return st;
+  if (!(sm_scale >= 0.f) || sm_scale > 1e30f)
+    return fail(MTS_ERR_INVALID_ARG, "sm_scale must be finite and >= 0 (0 selects 1/sqrt(D))");
+  if (b.batch == 0 || b.total_new == 0) return MTS_OK;
+  if (!q || !out) return fail(MTS_ERR_INVALID_ARG, "q / out is NULL");
+  if (!aligned(q, 16) || !aligned(out, 16)) return fail(MTS_ERR_INVALID_ARG, "q / out is not 16-byte aligned");
+  const mts::Q8AttnPlan plan = mts::plan_q8_attention(g, num_q_heads, b);
+  if (plan.too_large) return too_large_q8(b);
+  if (plan.ws_bytes > 0) {
+    if (!workspace) return fail(MTS_ERR_WORKSPACE, "workspace is NULL but %lld bytes are needed", (long long)plan.ws_bytes);
+    if (workspace_bytes < plan.ws_bytes)
+      return fail(MTS_ERR_WORKSPACE, "workspace has %lld bytes, %lld needed", (long long)workspace_bytes, (long long)plan.ws_bytes);
+    if (!aligned(workspace, 256)) return fail(MTS_ERR_WORKSPACE, "workspace is not 256-byte aligned");
+  }
+  const float scale = sm_scale > 0.f ? sm_scale : 1.0f / sqrtf((float)g.D);
+  return hip_status(mts::launch_q8_attn(g, plan, row_dtype == MTS_F32, num_q_heads, q, out, b, scale, workspace,
+                                        static_cast<hipStream_t>(stream)), "mts_attn_incremental_q8 launch");
+}
+
+// ---- norm and rotation of queries and keys ---------------------------------------------------------
+
+int32_t mts_qk_norm_rope(const mts_qk_desc* d, const void* q, const void* k, void* q_out, void* k_out, const mts_batch_meta* meta,
+                         void* stream) {
+  if (!d) return fail(MTS_ERR_INVALID_ARG, "descriptor is NULL");
+  int32_t st;
+  if ((st = check_row_type(d->dtype)) != MTS_OK) return st;
+  if (d->head_dim != 32 && d->head_dim != 64 && d->head_dim != 128)
+    return fail(MTS_ERR_UNSUPPORTED, "head_dim %d not in {32, 64, 128}", d->head_dim);
+  if (d->num_q_heads < 1 || d->num_q_heads > 65535 || d->num_k_heads < 1 || d->num_k_heads > 65535)
+    return fail(MTS_ERR_INVALID_ARG, "num_q_heads %d or num_k_heads %d out of range [1, 65535]", d->num_q_heads, d->num_k_heads);
+  if (d->norm != MTS_NORM_NONE && d->norm != MTS_NORM_RMS) return fail(MTS_ERR_UNSUPPORTED, "norm %d is no MTS_NORM_*", d->norm);
+  if (d->norm == MTS_NORM_RMS && !(d->eps >= 0.f && d->eps <= 1e30f)) return fail(MTS_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  if (d->pairs != MTS_ROPE_HALVES && d->pairs != MTS_ROPE_NEIGHBOURS) return fail(MTS_ERR_UNSUPPORTED, "pairs %d is no MTS_ROPE_*", d->pairs);
+  if (d->rot_dim < 0 || d->rot_dim > d->head_dim || d->rot_dim % 8)
+    return fail(MTS_ERR_SHAPE, "rot_dim %d is not a multiple of 8 in [0, head_dim %d]", d->rot_dim, d->head_dim);
+  if (d->rot_dim > 0 && !d->freqs) return fail(MTS_ERR_INVALID_ARG, "freqs is NULL");
+  if (!aligned(d->freqs, 8)) return fail(MTS_ERR_INVALID_ARG, "freqs is not 8-byte aligned");
+  if (!aligned(d->q_weight, 16) || !aligned(d->k_weight, 16)) return fail(MTS_ERR_INVALID_ARG, "q_weight / k_weight is not 16-byte aligned");
+  mts::QkArgs a{};
+  const int es = elem_bytes(d->dtype);
+  if ((st = row_stride("q_token_stride", d->q_token_stride, d->num_q_heads, d->head_dim, es, &a.q_stride)) != MTS_OK) return st;
+  if ((st = row_stride("k_token_stride", d->k_token_stride, d->num_k_heads, d->head_dim, es, &a.k_stride)) != MTS_OK) return st;
+  if ((st = row_stride("q_out_token_stride", d->q_out_token_stride, d->num_q_heads, d->head_dim, es, &a.q_out_stride)) != MTS_OK) return st;
+  if ((st = row_stride("k_out_token_stride", d->k_out_token_stride, d->num_k_heads, d->head_dim, es, &a.k_out_stride)) != MTS_OK) return st;
+  mts::BatchDev b{};
+  if ((st = check_meta(meta, true, false, &b)) != MTS_OK) return st;
+  if (b.batch == 0 || b.total_new == 0) return MTS_OK;
+  if (!b.prefix_lens || !b.new_indptr) return fail(MTS_ERR_INVALID_ARG, "prefix_lens / new_indptr is NULL");
+  if (!q || !k || !q_out || !k_out) return fail(MTS_ERR_INVALID_ARG, "q / k / q_out / k_out is NULL");
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(q_out, 16) || !aligned(k_out, 16))
+    return fail(MTS_ERR_INVALID_ARG, "q / k / q_out / k_out is not 16-byte aligned");
+  if (((int64_t)d->num_q_heads + d->num_k_heads) * b.total_new >= (1ll << 32))
+    return fail(MTS_ERR_UNSUPPORTED, "%d tokens of %d + %d heads are more rows than one call takes (2^32)", b.total_new, d->num_q_heads, d->num_k_heads);
+  a.q = (const char*)q; a.k = (const char*)k; a.q_out = (char*)q_out; a.k_out = (char*)k_out;
+  a.q_weight = (const char*)d->q_weight; a.k_weight = (const char*)d->k_weight; a.freqs = d->freqs; a.eps = d->eps;
+  a.Hq = d->num_q_heads; a.Hk = d->num_k_heads; a.D = d->head_dim; a.rot_dim = d->rot_dim;
+  a.f32 = d->dtype == MTS_F32; a.norm = d->norm == MTS_NORM_RMS; a.neighbours = d->pairs == MTS_ROPE_NEIGHBOURS;
+  return hip_status(mts::launch_qk_norm_rope(a, b, static_cast<hipStream_t>(stream)), "mts_qk_norm_rope launch");
 }
 
 int32_t mts_stage_h2d_async(void* device_dst, const void* host_src, int64_t bytes, void* stream) {

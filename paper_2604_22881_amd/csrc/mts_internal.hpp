@@ -9,6 +9,16 @@
 
 namespace mts {
 
+struct Q8Geom {              // the 8-bit pool (mts_q8.hpp)
+  char*   layer_base;
+  int64_t page_bytes;        // 2 * H * S * (D + 1)
+  int32_t num_pages;
+  int32_t S;
+  int32_t H;                 // key heads
+  int32_t D;
+  int32_t sub_shift;         // log2(S / 16)
+};
+
 // records the calling thread's error text (what mts_last_error returns) and returns `code`
 int32_t set_error(int32_t code, const char* fmt, ...);
 
@@ -131,5 +141,41 @@ hipError_t launch_attn_mfma(const PoolGeom& g, const AttnPlan& plan, const void*
                             const BatchDev& b, float sm_scale, float inv_norm, void* workspace,
                             hipStream_t stream, const void* k_new = nullptr, const void* v_new = nullptr,
                             const StagedHistories* hist = nullptr);
+
+// The 8-bit pool's operators.  f32: rows are float, else bf16; strides in bytes.
+hipError_t launch_q8_append(const Q8Geom& g, bool f32, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                            const BatchDev& b, hipStream_t stream);
+hipError_t launch_q8_unpack(const Q8Geom& g, bool f32, const void* staging, const SegDev& s, const BatchDev& b, hipStream_t stream);
+hipError_t launch_q8_pack(const Q8Geom& g, bool f32, void* staging_out, const SegDev& s, const BatchDev& b, hipStream_t stream);
+
+// Launch plan of one attention call over the 8-bit pool, from the scalar bounds only.
+struct Q8AttnPlan {
+  int32_t rows;              // query rows (tokens x query heads of a key head) of a tile: 16 or 32
+  int32_t q_tiles;           // tiles of the longest user's rows
+  int32_t chunk_shift;       // a user's keys are cut into chunks of 2^chunk_shift tokens; 31: not cut
+  int32_t part_rows;         // rows a chunk's partial result has room for
+  int64_t slots;             // chunks of all users, or some more
+  int64_t items;             // workgroups: slots * q_tiles * H
+  int64_t ws_bytes;
+  bool    too_large;
+};
+Q8AttnPlan plan_q8_attention(const Q8Geom& g, int32_t num_q_heads, const BatchDev& b);
+hipError_t launch_q8_attn(const Q8Geom& g, const Q8AttnPlan& plan, bool f32, int32_t num_q_heads, const void* q, void* out,
+                          const BatchDev& b, float sm_scale, void* workspace, hipStream_t stream);
+
+struct QkArgs {              // mts_qk_desc, checked, strides in bytes
+  const char*   q;
+  const char*   k;
+  char*         q_out;
+  char*         k_out;
+  int64_t       q_stride, k_stride, q_out_stride, k_out_stride;
+  const char*   q_weight;
+  const char*   k_weight;
+  const double* freqs;
+  float         eps;
+  int32_t       Hq, Hk, D, rot_dim;
+  bool          f32, norm, neighbours;
+};
+hipError_t launch_qk_norm_rope(const QkArgs& a, const BatchDev& b, hipStream_t stream);
 
 }  // namespace mts

@@ -18,12 +18,12 @@ class PagedKVCache:
 
     def __init__(self, layers, num_pages, page_size, heads, head_dim, dtype, device="cuda:0",
                  fill_byte=None):
-        self.dtype = dtype
-        es = 4 if dtype == "f32" else 2
-        self.desc = B.CacheDesc(None, 0, B.MTS_F32 if dtype == "f32" else B.MTS_BF16, layers,
+        self.dtype = dtype                    # "f32", "bf16" or "e4m3" (the pool of the *_q8 calls)
+        row_bytes = head_dim + 1 if dtype == "e4m3" else head_dim * (4 if dtype == "f32" else 2)
+        self.desc = B.CacheDesc(None, 0, {"f32": B.MTS_F32, "e4m3": B.MTS_E4M3}.get(dtype, B.MTS_BF16), layers,
                                 num_pages, page_size, heads, head_dim)
         self.page_bytes = B.mts_page_bytes(self.desc)
-        assert self.page_bytes == 2 * heads * page_size * head_dim * es
+        assert self.page_bytes == 2 * heads * page_size * row_bytes
         stride = (num_pages * self.page_bytes + 255) // 256 * 256
         self.pool = torch.empty(layers * stride, dtype=torch.uint8, device=device)
         if fill_byte is not None:
