@@ -150,7 +150,8 @@ hipError_t launch_q8_pack(const Q8Geom& g, bool f32, void* staging_out, const Se
 
 // Launch plan of one attention call over the 8-bit pool, from the scalar bounds only.
 struct Q8AttnPlan {
-  int32_t rows;              // query rows (tokens x query heads of a key head) of a tile: 16 or 32
+  int32_t rows;              // query rows (tokens x query heads of a key head) of a tile
+  bool    wide;              // the kernel for many rows
   int32_t q_tiles;           // tiles of the longest user's rows
   int32_t chunk_shift;       // a user's keys are cut into chunks of 2^chunk_shift tokens; 31: not cut
   int32_t part_rows;         // rows a chunk's partial result has room for

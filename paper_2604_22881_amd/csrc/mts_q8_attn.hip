@@ -44,6 +44,7 @@ constexpr float kRef = 10.f;       // log2 of the weight of the references
 constexpr float kMost = 15.f;      // of the largest weight (fp16 ends below 2^16)
 // A reference is a rounded logit, an fma's product is not: up to this size the two differ by 1/4 at most.
 constexpr float kFused = 4194304.f;
+constexpr float kNoExp = (float)(kQ8ExpMin + 127);   // what keys without a row count as
 constexpr float kLog2e = 1.44269504088896340736f;
 
 struct Q8AttnArgs {
@@ -99,48 +100,65 @@ __device__ __forceinline__ int keys_of(const UserSpan& s, int last_row, int G) {
   return min(s.prefix + min(last_row / G, kMostKeys - 1) + 1, s.held);
 }
 
+// The codes of one granule as a matrix operand: 8 dims of K times the row's power of two; 4 + 4 keys of V of one dim.
+__device__ __forceinline__ bf16x8 k_operand(uint32_t a, uint32_t b, float scale) {
+  u32x4 w;
+  w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false));
+  w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true));
+  w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false));
+  w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true));
+  return __builtin_bit_cast(bf16x8, w);
+}
+__device__ __forceinline__ u32x2 v_values(uint32_t a) {
+  return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, true))};
+}
+// byte r of a word of exponent bytes as e + 127 and as 2^-e
+__device__ __forceinline__ float exp_of(uint32_t w, int r) { return (float)((w >> (8 * r)) & 255u); }
+__device__ __forceinline__ float inverse_of(uint32_t w, int r) { return __uint_as_float((254u - ((w >> (8 * r)) & 255u)) << 23); }
+// 0xff where a byte is a NaN code
+__device__ __forceinline__ uint32_t nan_codes(uint32_t w) {
+  const uint32_t top = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+  return top | (top - (top >> 7));
+}
+
+// A wavefront's query rows and sums.
 template <int D, int MT, typename T>
 struct Attn {
   static constexpr int GB = D >= 64 ? 16 : 8;          // bytes of a lane's granule
   static constexpr int NJ = D >= 64 ? D / 64 : 1;      // granules of a row / 4
   static constexpr int NE = GB / 8;                    // matrix steps of a granule
+  static constexpr int KS = NJ * NE;
   static constexpr int W = GB / 4;                     // 16-dim tiles of a granule of V
   static constexpr int DT = D / 16;
   static constexpr bool kF32 = std::is_same<T, float>::value;
   static constexpr int QP = kF32 ? 3 : 1, PP = kF32 ? 2 : 1;
   using Granule = typename std::conditional<GB == 16, u32x4, u32x2>::type;
 
-  struct Tile {
-    Granule  k[2][NJ], v[2][NJ];
-    uint32_t ke[2], ve[2];
-  };
-
-  bf16x8 q[MT][NJ * NE][QP];
+  bf16x8 q[MT][KS][QP];
   f32x4  o[MT][DT];
-  float  neg_y[MT], l[MT];         // -(Y - kRef); sums of this lane's tokens
-  int    E;                        // reference of V's exponents, as byte
+  float  neg_y[MT];                // -(Y - kRef)
+  float  neg_r[MT];                // the same less E, for a fused subtraction
+  float  l[MT];                    // sums of this lane's keys, times 2^(-127 - E) ..
+  float  E;                        // reference of V's exponents, + 127
+  bool   first;                    // no keys yet
   bool   huge;                     // some reference is beyond what an fma may be exact to
 
-  static __device__ __forceinline__ bf16x8 k_operand(const Granule& g, int e, float scale) {
-    u32x4 w;
-    w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(g[2 * e], scale, false));
-    w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(g[2 * e], scale, true));
-    w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(g[2 * e + 1], scale, false));
-    w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(g[2 * e + 1], scale, true));
-    return __builtin_bit_cast(bf16x8, w);
-  }
-  static __device__ __forceinline__ f16x8 v_operand(uint32_t a, uint32_t b) {
-    u32x4 w;
-    w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, false));
-    w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, true));
-    w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, false));
-    w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, true));
-    return __builtin_bit_cast(f16x8, w);
+  __device__ __forceinline__ void start() {
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      neg_y[m] = neg_r[m] = l[m] = 0.f;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) o[m][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    E = kNoExp;
+    first = true;
+    huge = false;
   }
 
   __device__ __forceinline__ void load_queries(int mt, const char* row, int grp) {
 #pragma unroll
-    for (int s = 0; s < NJ * NE; ++s) {
+    for (int s = 0; s < KS; ++s) {
       const int d = (s / NE) * 4 * GB + grp * GB + (s % NE) * 8;
       if constexpr (kF32) {
         const f32x4 a = *reinterpret_cast<const f32x4*>(row + d * 4), b = *reinterpret_cast<const f32x4*>(row + d * 4 + 16);
@@ -160,89 +178,64 @@ struct Attn {
     }
   }
 
-  // Weights and sums of one tile of 32 keys, the first of them `key0`.  `edge`: some row does not see all of them; lim: the last
-  // key that this lane's query sees; key_end: the keys behind it were never written.
-  __device__ __forceinline__ void tile(Tile& t, int key0, bool edge, const int (&lim)[MT], int key_end, float scale, bool& first, int grp) {
+  // Weights and sums of one tile of 32 keys, the first of them `key0`.  k_op(h, s), v_op(c): the operands; ef, iv: e + 127 and
+  // 2^-e of this lane's keys of V.  `edge`: some row does not see all keys; lim: the last key that this lane's query sees.
+  template <typename K, typename V>
+  __device__ __forceinline__ void tile(K&& k_op, V&& v_op, const float (&ef)[2][4], const float (&iv)[2][4], int key0, bool edge,
+                                       const int (&lim)[MT], float scale, int grp) {
     f32x4 s[2][MT];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
 #pragma unroll
       for (int m = 0; m < MT; ++m) s[h][m] = f32x4{0.f, 0.f, 0.f, 0.f};
-      const float ks = __uint_as_float(t.ke[h] << 23);
 #pragma unroll
-      for (int j = 0; j < NJ; ++j)
+      for (int i = 0; i < KS; ++i) {
+        const bf16x8 k = k_op(h, i);
 #pragma unroll
-        for (int e = 0; e < NE; ++e) {
-          const bf16x8 k = k_operand(t.k[h][j], e, ks);
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-          for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int p = QP - 1; p >= 0; --p)
-              s[h][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[m][j * NE + e][p], s[h][m], 0, 0, 0);
-        }
-    }
-    if (edge) {
-      // what lies behind the last key is anything: exponents are given the reference's, codes 0
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int left = min(max(key_end - (key0 + 16 * h + 4 * grp), 0), 4);
-        const uint32_t keep = left == 4 ? ~0u : (1u << (8 * left)) - 1u;
-        t.ve[h] = (t.ve[h] & keep) | ((uint32_t)(first ? 67 : E) * 0x01010101u & ~keep);
-#pragma unroll
-        for (int j = 0; j < NJ; ++j)
-#pragma unroll
-          for (int w = 0; w < W; ++w) t.v[h][j][w] &= keep;
+          for (int p = QP - 1; p >= 0; --p) s[h][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[m][i][p], s[h][m], 0, 0, 0);
       }
     }
-    int  d[2][4];                              // E - e
-    float x[2][MT][4];
-    auto differences = [&] {
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) d[h][r] = E - (int)((t.ve[h] >> (8 * r)) & 255u);
-    };
+    float x[2][MT][4];                         // log2 of the weights
     auto hidden = [&](int h, int m, int r) { return edge && key0 + 16 * h + 4 * grp + r > lim[m]; };
-    auto weigh = [&](auto fused) {             // x: log2 of the weights
+    auto weigh = [&] {
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float y = decltype(fused)::value ? __builtin_fmaf(s[h][m][r], scale, neg_y[m]) : rounded_product(s[h][m][r], scale) + neg_y[m];
-            x[h][m][r] = hidden(h, m, r) ? -__builtin_inff() : y - (float)d[h][r];
-          }
+          for (int r = 0; r < 4; ++r) x[h][m][r] = __builtin_fmaf(s[h][m][r], scale, neg_r[m]) + ef[h][r];
     };
-    auto weigh_any = [&] {
-      if (huge) weigh(std::false_type{});
-      else weigh(std::true_type{});
+    auto hide = [&] {
+      if (edge) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[h][m][r] = hidden(h, m, r) ? -__builtin_inff() : x[h][m][r];
+      }
     };
-    bool over = first;
-    if (!first) {
-      differences();
-      weigh_any();
-      float most = -__builtin_inff();
+    weigh();
+    hide();
+    float most = -__builtin_inff();
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) most = fmaxf(most, x[h][m][r]);
-      over = __any(most > kMost);
-    }
-    if (over) {
-      // references that hold for this tile too, the sums scaled to them
-      int e_most = first ? 0 : E;
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) e_most = max(e_most, (int)((t.ve[h] >> (8 * r)) & 255u));
-      e_most = (int)over_groups((float)e_most, [](float a, float b) { return fmaxf(a, b); });
-      e_most = uniform_int(e_most);
-      const float e_step = __uint_as_float((uint32_t)max(127 + (first ? 0 : E - e_most), 0) << 23);
+        for (int r = 0; r < 4; ++r) most = fmaxf(most, x[h][m][r]);
+    if (first || huge || __any(most > kMost)) {
+      // references that hold for this tile too, the sums scaled to them
+      float e_most = E;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) e_most = fmaxf(e_most, ef[h][r]);
+      e_most = over_groups(e_most, [](float a, float b) { return fmaxf(a, b); });
+      const float e_step = exp2_of(E - e_most);
       E = e_most;
-      differences();
       float largest = 0.f;
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
@@ -256,16 +249,27 @@ struct Attn {
         const float was = neg_y[m];
         const bool seen = y > -__builtin_inff();
         const float now = seen ? (first ? kRef - y : fminf(was, kRef - y)) : was;
-        const float f = first ? 0.f : exp2_of(now - was);
+        const float f = first ? 0.f : exp2_of(now - was) * e_step;
         neg_y[m] = now;
+        neg_r[m] = now - E;
         l[m] *= f;
 #pragma unroll
-        for (int c = 0; c < DT; ++c) o[m][c] *= f * e_step;
+        for (int c = 0; c < DT; ++c) o[m][c] *= f;
         largest = fmaxf(largest, __builtin_fabsf(now));
       }
       huge = __any(largest > kFused);
-      weigh_any();
       first = false;
+      if (huge) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[h][m][r] = (rounded_product(s[h][m][r], scale) + neg_y[m]) + (ef[h][r] - E);
+      } else {
+        weigh();
+      }
+      hide();
     }
     f16x8 p[MT][PP];
 #pragma unroll
@@ -276,7 +280,7 @@ struct Attn {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           w[r] = exp2_of(x[h][m][r]);
-          l[m] = __builtin_fmaf(w[r], __uint_as_float((uint32_t)(d[h][r] + 127) << 23), l[m]);
+          l[m] = __builtin_fmaf(w[r], iv[h][r], l[m]);
         }
 #pragma unroll
         for (int r = 0; r < 4; r += 2) {
@@ -291,134 +295,222 @@ struct Attn {
         }
       }
     }
-    bool poisoned = false;
-    if (edge) {
-      // a NaN in V of a key that some rows see and others do not must not reach the others through 0 * NaN
-      uint32_t nan = 0;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+    for (int c = 0; c < DT; ++c) {
+      const f16x8 v = v_op(c);
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
+      for (int m = 0; m < MT; ++m)
 #pragma unroll
-          for (int w = 0; w < W; ++w) nan |= (t.v[h][j][w] & 0x7f7f7f7fu) + 0x01010101u;
-      poisoned = __any((nan & 0x80808080u) != 0);
+        for (int i = PP - 1; i >= 0; --i) o[m][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[m][i], o[m][c], 0, 0, 0);
     }
-    if (poisoned) {
-      // one key at a time: its column alone, and its product only for the queries that see it
+  }
+
+  // NaN in V among keys that not all rows see: their codes were left out of the products (0 * NaN would reach every row), and are
+  // brought in here, key by key for the queries that see it.  v: the codes of the lane's granules, of both sub-blocks.
+  __device__ __forceinline__ void add_nan(const Granule (&v)[2][NJ], int key0, const int (&lim)[MT], int grp) {
 #pragma unroll 1
-      for (int key = 0; key < 32; ++key) {
-        const int h = key >> 4, g = (key >> 2) & 3, r = key & 3;
-        const uint32_t keep = grp == g ? 0xffu << (8 * r) : 0u;
-        const uint32_t k0 = h == 0 ? keep : 0u, k1 = h == 1 ? keep : 0u;
-#pragma unroll
-        for (int c = 0; c < DT; ++c) {
-          const f16x8 v = v_operand(t.v[0][c / W][c % W] & k0, t.v[1][c / W][c % W] & k1);
-#pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            f32x4 n = o[m][c];
-#pragma unroll
-            for (int i = 0; i < PP; ++i) n = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[m][i], n, 0, 0, 0);
-            o[m][c] = key0 + key <= lim[m] ? n : o[m][c];
-          }
-        }
-      }
-    } else {
+    for (int key = 0; key < 32; ++key) {
+      const bool mine = grp == ((key >> 2) & 3);
+      uint32_t byte[DT], any = 0;
 #pragma unroll
       for (int c = 0; c < DT; ++c) {
-        const f16x8 v = v_operand(t.v[0][c / W][c % W], t.v[1][c / W][c % W]);
+        byte[c] = ((key < 16 ? v[0][c / W][c % W] : v[1][c / W][c % W]) >> (8 * (key & 3))) & 0x7fu;
+        any |= mine && byte[c] == 0x7fu;
+      }
+      if (!__any(any)) continue;
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+      for (int c = 0; c < DT; ++c) {
+        const u32x4 a{mine && byte[c] == 0x7fu ? 0x7e00u : 0u, 0u, 0u, 0u}, one{0x3c00u, 0u, 0u, 0u};
 #pragma unroll
-          for (int i = PP - 1; i >= 0; --i) o[m][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[m][i], o[m][c], 0, 0, 0);
+        for (int m = 0; m < MT; ++m) {
+          const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, one), o[m][c], 0, 0, 0);
+          o[m][c] = key0 + key <= lim[m] ? n : o[m][c];
+        }
       }
     }
   }
+
+  // sum of the weights over all keys, in units of the output's
+  __device__ __forceinline__ float total(int m) const {
+    return over_groups(l[m], [](float a, float b) { return a + b; }) * exp2_of(E - 127.f);
+  }
 };
 
+// bytes of the first n of four keys
+__device__ __forceinline__ uint32_t first_bytes(int n) { return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1u; }
+
+// What a workgroup is to do: a tile of M rows of user u's head h from row_first on, keys [key_first, key_last).
+struct Work {
+  UserSpan us;
+  int64_t  item;
+  int      h, row_first, row_last;
+  int      key_first, key_last;
+  int      keys;                   // of the whole tile of rows
+  bool     partial;                // one of several stretches
+};
+template <int M, bool SPLIT>
+__device__ __forceinline__ bool find_work(const Q8AttnArgs& a, int64_t slot, int qt, int h, Work& w) {
+  int u = (int)slot;
+  w.key_first = 0;
+  auto base = [&](int s) -> int64_t { return (((int64_t)a.b.page_indptr[s] * a.g.S) >> a.chunk_shift) + s; };
+  if constexpr (SPLIT) {
+    u = find_user(a.b.batch, slot, base);
+    const int64_t chunk = slot - base(u);
+    if (chunk < 0 || chunk > (kMostKeys >> a.chunk_shift)) return false;
+    w.key_first = (int)(chunk << a.chunk_shift);
+  }
+  w.us = user_span(a.b, a.g.S, u);
+  const int64_t rows = (int64_t)w.us.n * a.G, first = (int64_t)qt * M;
+  if (first >= rows) return false;
+  w.h = h;
+  w.row_first = (int)first;
+  w.row_last = (int)(first + M < rows ? first + M : rows) - 1;
+  w.keys = keys_of(w.us, w.row_last, a.G);
+  if (w.key_first >= w.keys) return false;
+  w.partial = SPLIT && w.keys > (1 << a.chunk_shift);
+  w.key_last = w.partial ? min(w.key_first + (1 << a.chunk_shift), w.keys) : w.keys;
+  w.item = (slot * a.q_tiles + qt) * a.g.H + h;
+  return true;
+}
+// index of a query row among [total_new][Hq]
+__device__ __forceinline__ int64_t row_at(const Q8AttnArgs& a, const Work& w, int row) {
+  return ((int64_t)(w.us.row0 + row / a.G) * a.g.H + w.h) * a.G + row % a.G;
+}
+// Codes and exponents of a 16-token sub-block of the head; those behind the last one, and those of a page that is none, are
+// another's.
+template <int D>
+struct SubBlock {
+  const char *k, *v, *ke, *ve;
+  __device__ __forceinline__ SubBlock(const Q8AttnArgs& a, uint32_t id, int64_t head_off, int in_page) {
+    const int64_t page = id < (uint32_t)a.g.num_pages ? id : 0;
+    const char* head = a.g.layer_base + page * a.g.page_bytes + head_off;
+    k = head + in_page * 16 * D;
+    v = k + a.g.S * D;
+    ke = head + 2 * a.g.S * D + in_page * 16;
+    ve = ke + a.g.S;
+  }
+};
+// Four dims, from d on, of a row's result or, `partial`, of its stretch.
+template <int D, typename T>
+__device__ __forceinline__ void store_sums(const Q8AttnArgs& a, const Work& w, int row, int d, f32x4 v, float inv) {
+  if (w.partial) {
+    *reinterpret_cast<f32x4*>(a.part_o + (w.item * a.part_rows + (row - w.row_first)) * D + d) = v;
+    return;
+  }
+  v *= inv;
+  const int64_t at = row_at(a, w, row) * D + d;
+  if constexpr (std::is_same<T, float>::value) {
+    *reinterpret_cast<f32x4*>(a.out + at * 4) = v;
+  } else {
+    const bf16x2 lo = __builtin_convertvector((f32x2{v[0], v[1]}), bf16x2), hi = __builtin_convertvector((f32x2{v[2], v[3]}), bf16x2);
+    *reinterpret_cast<u32x2*>(a.out + at * 2) = u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+  }
+}
+
+// Few rows: every wavefront has all of them and every fourth tile of the keys.
 template <int D, int MT, typename T, bool SPLIT>
 __global__ __launch_bounds__(256, D == 128 || MT == 2 ? 2 : 3) void q8_attn_kernel(Q8AttnArgs a) {
   using A = Attn<D, MT, T>;
   constexpr int M = 16 * MT;
   const int lane = threadIdx.x & 63, grp = lane >> 4, wave = uniform_int(threadIdx.x >> 6);
-  const int h = blockIdx.x % a.g.H;
-  const int64_t rest = blockIdx.x / a.g.H;
-  const int qt = (int)(rest % a.q_tiles);
-  const int64_t slot = rest / a.q_tiles;
-  int u = (int)slot, key_first = 0;
-  auto base = [&](int s) -> int64_t { return (((int64_t)a.b.page_indptr[s] * a.g.S) >> a.chunk_shift) + s; };
-  if constexpr (SPLIT) {
-    u = find_user(a.b.batch, slot, base);
-    const int64_t chunk = slot - base(u);
-    if (chunk < 0 || chunk > (kMostKeys >> a.chunk_shift)) return;
-    key_first = (int)(chunk << a.chunk_shift);
-  }
-  const UserSpan us = user_span(a.b, a.g.S, u);
-  const int64_t rows = (int64_t)us.n * a.G, row_first = (int64_t)qt * M;
-  if (row_first >= rows) return;
-  const int row_last = (int)(row_first + M < rows ? row_first + M : rows) - 1;
-  const int keys = keys_of(us, row_last, a.G);
-  if (SPLIT && key_first >= keys) return;
-  const bool partial = SPLIT && keys > (1 << a.chunk_shift);
-  const int key_last = partial ? min(key_first + (1 << a.chunk_shift), keys) : keys;   // one behind
-  const int all_see = us.prefix + (int)(row_first / a.G);    // the last key that every row sees
+  const uint32_t rest = blockIdx.x / (uint32_t)a.g.H;
+  Work wk;
+  if (!find_work<M, SPLIT>(a, rest / (uint32_t)a.q_tiles, (int)(rest % (uint32_t)a.q_tiles), (int)(blockIdx.x % (uint32_t)a.g.H), wk)) return;
+  const int all_see = wk.us.prefix + wk.row_first / a.G;     // the last key that every row sees
 
   A c;
+  c.start();
   int lim[MT];
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
-    const int64_t r = row_first + 16 * m + (lane & 15);
-    const int row = (int)(r < row_last ? r : row_last);      // rows behind the last repeat it and are not stored
-    lim[m] = us.prefix + row / a.G;
-    const int64_t at = ((int64_t)(us.row0 + row / a.G) * a.g.H + h) * a.G + row % a.G;
-    c.load_queries(m, a.q + at * D * (int64_t)sizeof(T), grp);
-    c.neg_y[m] = 0.f;
-    c.l[m] = 0.f;
-#pragma unroll
-    for (int i = 0; i < A::DT; ++i) c.o[m][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int row = min(wk.row_first + 16 * m + (lane & 15), wk.row_last);   // rows behind the last repeat it and are not stored
+    lim[m] = wk.us.prefix + row / a.G;
+    c.load_queries(m, a.q + row_at(a, wk, row) * D * (int64_t)sizeof(T), grp);
   }
-  c.E = 67;
-  c.huge = false;
-  bool first = true;
 
-  const int64_t head_off = h * q8_head_bytes(a.g.S, D);
+  struct Tile {
+    typename A::Granule k[2][A::NJ], v[2][A::NJ];
+    uint32_t ke[2], ve[2];
+  };
+  const int64_t head_off = wk.h * q8_head_bytes(a.g.S, D);
   const int sub_mask = (1 << a.g.sub_shift) - 1;
-  const int last_sub = (keys + 15) / 16 - 1;
-  const int* pages = a.b.page_indices + us.page0;
-  auto load = [&](typename A::Tile& t, int tile) {
+  const int last_sub = (wk.keys + 15) / 16 - 1;
+  const int* pages = a.b.page_indices + wk.us.page0;
+  auto load = [&](Tile& t, int tile) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       const int sub = min(2 * tile + s, last_sub);
-      const uint32_t id = (uint32_t)uniform_int(pages[sub >> a.g.sub_shift]);
-      const int64_t page = id < (uint32_t)a.g.num_pages ? id : 0;
-      const char* head = a.g.layer_base + page * a.g.page_bytes + head_off;
-      const int in_page = sub & sub_mask;
-      const char* kc = head + in_page * 16 * D;
-      const char* vc = kc + a.g.S * D;
-      const char* ex = head + 2 * a.g.S * D + in_page * 16;
+      const SubBlock<D> at(a, (uint32_t)uniform_int(pages[sub >> a.g.sub_shift]), head_off, sub & sub_mask);
 #pragma unroll
       for (int j = 0; j < A::NJ; ++j) {
-        t.k[s][j] = *reinterpret_cast<const typename A::Granule*>(kc + j * 1024 + lane * A::GB);
-        t.v[s][j] = *reinterpret_cast<const typename A::Granule*>(vc + j * 1024 + lane * A::GB);
+        t.k[s][j] = *reinterpret_cast<const typename A::Granule*>(at.k + j * 1024 + lane * A::GB);
+        t.v[s][j] = *reinterpret_cast<const typename A::Granule*>(at.v + j * 1024 + lane * A::GB);
       }
-      t.ke[s] = *reinterpret_cast<const uint8_t*>(ex + (lane & 15));
-      t.ve[s] = *reinterpret_cast<const uint32_t*>(ex + a.g.S + 4 * grp);
+      t.ke[s] = *reinterpret_cast<const uint8_t*>(at.ke + (lane & 15));
+      t.ve[s] = *reinterpret_cast<const uint32_t*>(at.ve + 4 * grp);
     }
   };
-  const int tile_end = (key_last + 31) / 32;
-  int tile = key_first / 32 + wave;
+  uint32_t nan_seen = 0;
+  auto compute = [&](Tile& t, int tile) {
+    const int key0 = tile * 32;
+    const bool edge = key0 + 31 > all_see;
+    if (edge) {
+      // what lies behind the last key is anything
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const uint32_t keep = first_bytes(wk.key_last - (key0 + 16 * s + 4 * grp));
+        t.ve[s] = (t.ve[s] & keep) | ((uint32_t)kNoExp * 0x01010101u & ~keep);
+#pragma unroll
+        for (int j = 0; j < A::NJ; ++j)
+#pragma unroll
+          for (int w = 0; w < A::W; ++w) {
+            const uint32_t v = t.v[s][j][w] & keep, nan = nan_codes(v);
+            t.v[s][j][w] = v & ~nan;
+            nan_seen |= nan;
+          }
+      }
+    }
+    float ef[2][4], iv[2][4];
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) { ef[s][r] = exp_of(t.ve[s], r); iv[s][r] = inverse_of(t.ve[s], r); }
+    const float ks[2] = {__uint_as_float(t.ke[0] << 23), __uint_as_float(t.ke[1] << 23)};
+    c.tile([&](int h, int i) { return k_operand(t.k[h][i / A::NE][2 * (i % A::NE)], t.k[h][i / A::NE][2 * (i % A::NE) + 1], ks[h]); },
+           [&](int i) {
+             const u32x2 p = v_values(t.v[0][i / A::W][i % A::W]), q = v_values(t.v[1][i / A::W][i % A::W]);
+             return __builtin_bit_cast(f16x8, (u32x4{p[0], p[1], q[0], q[1]}));
+           }, ef, iv, key0, edge, lim, a.scale, grp);
+  };
+  const int tile_end = (wk.key_last + 31) / 32;
+  int tile = wk.key_first / 32 + wave;
   if (tile < tile_end) {
-    typename A::Tile t0, t1;
+    Tile t0, t1;
     load(t0, tile);
     for (;;) {
       const int next = tile + 4;
       load(t1, next < tile_end ? next : tile);
-      c.tile(t0, tile * 32, tile * 32 + 31 > all_see, lim, key_last, a.scale, first, grp);
+      compute(t0, tile);
       if (next >= tile_end) break;
       tile = next + 4;
       load(t0, tile < tile_end ? tile : next);
-      c.tile(t1, next * 32, next * 32 + 31 > all_see, lim, key_last, a.scale, first, grp);
+      compute(t1, next);
       if (tile >= tile_end) break;
     }
+  }
+  if (__any(nan_seen != 0)) {
+    for (int again = wk.key_first / 32 + wave; again < tile_end; again += 4)
+      if (again * 32 + 31 > all_see) {
+        Tile t;
+        load(t, again);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int j = 0; j < A::NJ; ++j)
+#pragma unroll
+            for (int w = 0; w < A::W; ++w) t.v[s][j][w] &= first_bytes(wk.key_last - (again * 32 + 16 * s + 4 * grp));
+        c.add_nan(t.v, again * 32, lim, grp);
+      }
   }
 
   // The four wavefronts' sums: each takes a quarter of the dims (of 32 dims two take half) from the others.
@@ -427,13 +519,13 @@ __global__ __launch_bounds__(256, D == 128 || MT == 2 ? 2 : 3) void q8_attn_kern
   __shared__ float xy[4][M], xl[4][M], xe[4];
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
-    const float l = over_groups(c.l[m], [](float p, float q) { return p + q; });
+    const float l = c.total(m);
     if (grp == 0) {
       xy[wave][16 * m + lane] = l == 0.f ? -__builtin_inff() : kRef - c.neg_y[m];   // none of its keys seen
       xl[wave][16 * m + lane] = l;
     }
   }
-  if (lane == 0) xe[wave] = (float)(c.E - 127);
+  if (lane == 0) xe[wave] = c.E - 127.f;
 #pragma unroll
   for (int w = 0; w < OWNERS; ++w)
     if (w != wave) {
@@ -445,10 +537,9 @@ __global__ __launch_bounds__(256, D == 128 || MT == 2 ? 2 : 3) void q8_attn_kern
     }
   __syncthreads();
   if (wave >= OWNERS) return;
-  const int64_t item = blockIdx.x;
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
-    const int in_tile = 16 * m + (lane & 15);
+    const int in_tile = 16 * m + (lane & 15), row = wk.row_first + in_tile;
     float y = xy[0][in_tile];
 #pragma unroll
     for (int w = 1; w < 4; ++w) y = fmaxf(y, xy[w][in_tile]);
@@ -460,8 +551,6 @@ __global__ __launch_bounds__(256, D == 128 || MT == 2 ? 2 : 3) void q8_attn_kern
       l = __builtin_fmaf(xl[w][in_tile], f[w], l);
       f[w] *= exp2_of(xe[w]);
     }
-    const int64_t r = row_first + in_tile;
-    const bool live = r <= row_last;
     const float inv = 1.f / l;
 #pragma unroll
     for (int i = 0; i < OWN; ++i) {
@@ -472,31 +561,165 @@ __global__ __launch_bounds__(256, D == 128 || MT == 2 ? 2 : 3) void q8_attn_kern
         if (w == wave) {
           p = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int cc = 0; cc < OWNERS; ++cc)
-            if (cc == wave) p = c.o[m][cc * OWN + i];
+          for (int o = 0; o < OWNERS; ++o)
+            if (o == wave) p = c.o[m][o * OWN + i];
         } else {
           p = xo[(((wave * 3 + w - (w > wave)) * OWN + i) * MT + m) * 64 + lane];
         }
         v += p * f[w];
       }
-      const int d = 16 * (wave * OWN + i) + 4 * grp;
-      if (live) {
-        if (partial) {
-          *reinterpret_cast<f32x4*>(a.part_o + (item * a.part_rows + in_tile) * D + d) = v;
-        } else {
-          v *= inv;
-          const int row = (int)r;
-          const int64_t at = ((int64_t)(us.row0 + row / a.G) * a.g.H + h) * a.G + row % a.G;
-          if constexpr (A::kF32) {
-            *reinterpret_cast<f32x4*>(a.out + (at * D + d) * 4) = v;
-          } else {
-            const bf16x2 lo = __builtin_convertvector((f32x2{v[0], v[1]}), bf16x2), hi = __builtin_convertvector((f32x2{v[2], v[3]}), bf16x2);
-            *reinterpret_cast<u32x2*>(a.out + (at * D + d) * 2) = u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+      if (row <= wk.row_last) store_sums<D, T>(a, wk, row, 16 * (wave * OWN + i) + 4 * grp, v, inv);
+    }
+    if (wk.partial && row <= wk.row_last && wave == 0 && grp == 0)
+      *reinterpret_cast<f32x2*>(a.part_ml + (wk.item * a.part_rows + in_tile) * 2) = f32x2{y, l};
+  }
+}
+
+// Many rows: the wavefronts have 16 MT rows each and go through the keys together.  A tile of 32 keys is converted to operands
+// once, a quarter by each wavefront, into one of two stages in LDS, while the other is multiplied from.
+template <int D, int MT, typename T, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void q8_attn_wide_kernel(Q8AttnArgs a) {
+  using A = Attn<D, MT, T>;
+  constexpr int M = 64 * MT;
+  struct Stage {
+    u32x4 k[2][A::KS][64];         // operands, one per lane
+    u32x4 v[A::DT][64];
+    float ef[2][16], iv[2][16];
+  };
+  __shared__ Stage stage[2];
+  __shared__ int nan_seen[2];
+  const int lane = threadIdx.x & 63, grp = lane >> 4, wave = uniform_int(threadIdx.x >> 6);
+  // Workgroups go to the 8 XCDs in turn; the tiles of one (user, head) share its keys in one XCD's L2: eight pairs at a time, a pair
+  // per XCD, the longest tiles first.
+  const uint32_t pairs = (uint32_t)(a.slots * a.g.H), per8 = 8u * (uint32_t)a.q_tiles;
+  const uint32_t eight = blockIdx.x / per8, in8 = blockIdx.x % per8, left = min(8u, pairs - 8u * eight);
+  const uint32_t pair = 8u * eight + in8 % left;
+  Work wk;
+  if (!find_work<M, SPLIT>(a, pair / (uint32_t)a.g.H, a.q_tiles - 1 - (int)(in8 / left), (int)(pair % (uint32_t)a.g.H), wk)) return;
+
+  A c;
+  c.start();
+  const int first_row = wk.row_first + 16 * MT * wave, last_row = min(first_row + 16 * MT - 1, wk.row_last);
+  const int all_rows_see = wk.us.prefix + wk.row_first / a.G;
+  const int all_see = wk.us.prefix + first_row / a.G, some_see = first_row <= wk.row_last ? wk.us.prefix + last_row / a.G : -1;
+  int lim[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const int row = min(first_row + 16 * m + (lane & 15), wk.row_last);
+    lim[m] = wk.us.prefix + row / a.G;
+    c.load_queries(m, a.q + row_at(a, wk, row) * D * (int64_t)sizeof(T), grp);
+  }
+
+  // this wavefront's part of a tile: K (0, 1) or V (2, 3) of one of the two sub-blocks
+  const int my_sub = wave & 1;
+  const bool is_v = wave >= 2;
+  const int64_t head_off = wk.h * q8_head_bytes(a.g.S, D);
+  const int sub_mask = (1 << a.g.sub_shift) - 1;
+  const int last_sub = (wk.keys + 15) / 16 - 1;
+  const int* pages = a.b.page_indices + wk.us.page0;
+  struct Raw {
+    typename A::Granule g[A::NJ];
+    uint32_t e;
+  };
+  auto sub_of = [&](int tile) { return min(2 * tile + my_sub, last_sub); };
+  auto load = [&](Raw& r, int tile, int id) {
+    const SubBlock<D> at(a, (uint32_t)id, head_off, sub_of(tile) & sub_mask);
+#pragma unroll
+    for (int j = 0; j < A::NJ; ++j) r.g[j] = *reinterpret_cast<const typename A::Granule*>((is_v ? at.v : at.k) + j * 1024 + lane * A::GB);
+    r.e = *reinterpret_cast<const uint8_t*>((is_v ? at.ve : at.ke) + (lane & 15));
+  };
+  auto page_of = [&](int tile) { return uniform_int(pages[sub_of(tile) >> a.g.sub_shift]); };
+  auto convert = [&](Raw& r, int tile, Stage& st) {
+    if (is_v) {
+      const int key0 = tile * 32 + 16 * my_sub;
+      if (tile * 32 + 31 > all_rows_see) {
+        const uint32_t keep = first_bytes(wk.key_last - (key0 + 4 * grp));
+        uint32_t any = 0;
+#pragma unroll
+        for (int j = 0; j < A::NJ; ++j)
+#pragma unroll
+          for (int w = 0; w < A::W; ++w) {
+            const uint32_t v = r.g[j][w] & keep, nan = nan_codes(v);
+            r.g[j][w] = v & ~nan;
+            any |= nan;
+          }
+        if (any) nan_seen[my_sub] = 1;
+        r.e = key0 + (lane & 15) < wk.key_last ? r.e : (uint32_t)kNoExp;
+      }
+#pragma unroll
+      for (int j = 0; j < A::NJ; ++j)
+#pragma unroll
+        for (int w = 0; w < A::W; ++w) reinterpret_cast<u32x2*>(&st.v[j * A::W + w][lane])[my_sub] = v_values(r.g[j][w]);
+      if (lane < 16) {
+        st.ef[my_sub][lane] = (float)r.e;
+        st.iv[my_sub][lane] = inverse_of(r.e, 0);
+      }
+    } else {
+      const float scale = __uint_as_float(r.e << 23);
+#pragma unroll
+      for (int i = 0; i < A::KS; ++i)
+        st.k[my_sub][i][lane] = __builtin_bit_cast(u32x4, k_operand(r.g[i / A::NE][2 * (i % A::NE)], r.g[i / A::NE][2 * (i % A::NE) + 1], scale));
+    }
+  };
+  const int tile_end = (wk.key_last + 31) / 32, tile_first = wk.key_first / 32;
+  if (threadIdx.x < 2) nan_seen[threadIdx.x] = 0;
+  __syncthreads();
+  Raw raw;
+  load(raw, tile_first, page_of(tile_first));
+  convert(raw, tile_first, stage[0]);
+  load(raw, tile_first + 1, page_of(tile_first + 1));
+  int id = page_of(tile_first + 2);
+  __syncthreads();
+  for (int tile = tile_first; tile < tile_end; ++tile) {
+    Stage& st = stage[(tile - tile_first) & 1];
+    if (tile + 1 < tile_end) {
+      convert(raw, tile + 1, stage[(tile + 1 - tile_first) & 1]);
+      load(raw, tile + 2, id);
+      id = page_of(tile + 3);
+    }
+    const int key0 = tile * 32;
+    if (key0 <= some_see) {
+      const bool edge = key0 + 31 > all_see;
+      float ef[2][4], iv[2][4];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const f32x4 e = *reinterpret_cast<const f32x4*>(&st.ef[h][4 * grp]), i = *reinterpret_cast<const f32x4*>(&st.iv[h][4 * grp]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) { ef[h][r] = e[r]; iv[h][r] = i[r]; }
+      }
+      c.tile([&](int h, int i) { return __builtin_bit_cast(bf16x8, st.k[h][i][lane]); },
+             [&](int i) { return __builtin_bit_cast(f16x8, st.v[i][lane]); }, ef, iv, key0, edge, lim, a.scale, grp);
+    }
+    __syncthreads();
+  }
+  if (uniform_int(nan_seen[0] | nan_seen[1]) != 0) {
+    for (int again = tile_first; again < tile_end; ++again)
+      if (again * 32 + 31 > all_rows_see) {
+        typename A::Granule v[2][A::NJ];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const int sub = min(2 * again + s, last_sub);
+          const SubBlock<D> at(a, (uint32_t)uniform_int(pages[sub >> a.g.sub_shift]), head_off, sub & sub_mask);
+          const uint32_t keep = first_bytes(wk.key_last - (again * 32 + 16 * s + 4 * grp));
+#pragma unroll
+          for (int j = 0; j < A::NJ; ++j) {
+            v[s][j] = *reinterpret_cast<const typename A::Granule*>(at.v + j * 1024 + lane * A::GB);
+#pragma unroll
+            for (int w = 0; w < A::W; ++w) v[s][j][w] &= keep;
           }
         }
+        c.add_nan(v, again * 32, lim, grp);
       }
-    }
-    if (partial && live && wave == 0 && grp == 0) *reinterpret_cast<f32x2*>(a.part_ml + (item * a.part_rows + in_tile) * 2) = f32x2{y, l};
+  }
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const float l = c.total(m), e = exp2_of(c.E - 127.f);
+    const int row = first_row + 16 * m + (lane & 15);
+    if (row > wk.row_last) continue;
+#pragma unroll
+    for (int i = 0; i < A::DT; ++i) store_sums<D, T>(a, wk, row, 16 * i + 4 * grp, c.o[m][i] * e, 1.f / l);
+    if (wk.partial && grp == 0)
+      *reinterpret_cast<f32x2*>(a.part_ml + (wk.item * a.part_rows + (row - wk.row_first)) * 2) = f32x2{l == 0.f ? -__builtin_inff() : kRef - c.neg_y[m], l};
   }
 }
 
@@ -556,7 +779,8 @@ __global__ __launch_bounds__(256) void q8_join_kernel(Q8AttnArgs a, int tile_row
 Q8AttnPlan plan_q8_attention(const Q8Geom& g, int32_t num_q_heads, const BatchDev& b) {
   Q8AttnPlan p{};
   const int64_t G = num_q_heads / g.H, rows = G * b.max_new;
-  p.rows = rows > 16 ? 32 : 16;
+  p.wide = rows >= 128;
+  p.rows = p.wide ? 128 : rows > 16 ? 32 : 16;
   p.q_tiles = (int)((rows + p.rows - 1) / p.rows);
   p.chunk_shift = 31;
   p.part_rows = (int)(rows < p.rows ? rows : p.rows);
@@ -584,7 +808,10 @@ template <int D, typename T>
 static hipError_t launch(const Q8AttnArgs& a, const Q8AttnPlan& p, hipStream_t stream) {
   const dim3 grid((unsigned)p.items), block(256);
   const bool split = p.chunk_shift < 31;
-  if (p.rows == 16) {
+  if (p.wide) {
+    if (split) q8_attn_wide_kernel<D, 2, T, true><<<grid, block, 0, stream>>>(a);
+    else q8_attn_wide_kernel<D, 2, T, false><<<grid, block, 0, stream>>>(a);
+  } else if (p.rows == 16) {
     if (split) q8_attn_kernel<D, 1, T, true><<<grid, block, 0, stream>>>(a);
     else q8_attn_kernel<D, 1, T, false><<<grid, block, 0, stream>>>(a);
   } else {
