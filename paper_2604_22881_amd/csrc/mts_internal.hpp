@@ -149,16 +149,21 @@ hipError_t launch_q8_unpack(const Q8Geom& g, bool f32, const void* staging, cons
 hipError_t launch_q8_pack(const Q8Geom& g, bool f32, void* staging_out, const SegDev& s, const BatchDev& b, hipStream_t stream);
 
 // Launch plan of one attention call over the 8-bit pool, from the scalar bounds only.
-struct Q8AttnPlan {
+struct Q8AttnLaunch {
+  bool    on;
   int32_t rows;              // query rows (tokens x query heads of a key head) of a tile
-  bool    wide;              // the kernel for many rows
-  int32_t q_tiles;           // tiles of the longest user's rows
-  int32_t chunk_shift;       // a user's keys are cut into chunks of 2^chunk_shift tokens; 31: not cut
-  int32_t part_rows;         // rows a chunk's partial result has room for
-  int64_t slots;             // chunks of all users, or some more
-  int64_t items;             // workgroups: slots * q_tiles * H
-  int64_t ws_bytes;
-  bool    too_large;
+  int32_t above, upto;       // takes the users with more query rows than that, and at most so many
+  int32_t q_tiles;           // few rows: tiles of the longest user's rows; many: stretches of the longest user's keys
+  int32_t tiles_each;        // many rows, users of one length: tiles of a user's; 0: by the table
+  int32_t chunk_shift;       // keys are cut into stretches of 2^chunk_shift tokens; 31: not cut
+  int32_t part_rows;         // rows a stretch's partial result has room for
+  int64_t slots;             // few rows: users, or stretches of all users; many: tiles of all users
+  int64_t items;             // workgroups
+};
+struct Q8AttnPlan {
+  Q8AttnLaunch wide, few;    // one after the other, in the same workspace
+  int64_t      ws_bytes;
+  bool         too_large;
 };
 Q8AttnPlan plan_q8_attention(const Q8Geom& g, int32_t num_q_heads, const BatchDev& b);
 hipError_t launch_q8_attn(const Q8Geom& g, const Q8AttnPlan& plan, bool f32, int32_t num_q_heads, const void* q, void* out,

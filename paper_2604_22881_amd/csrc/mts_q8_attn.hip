@@ -54,11 +54,14 @@ struct Q8AttnArgs {
   BatchDev    b;
   float       scale;               // sm_scale * log2(e)
   int32_t     G;                   // query heads of a key head
+  // of the launch, as in Q8AttnLaunch
+  int32_t     above, upto;
   int32_t     q_tiles;
+  int32_t     tiles_each;
   int32_t     chunk_shift;
   int32_t     part_rows;
   int64_t     slots;
-  float*      part_o;              // [item][part_rows][D], item = (slot * q_tiles + q tile) * H + head
+  float*      part_o;              // [item][part_rows][D]
   float*      part_ml;             // [item][part_rows][2]
 };
 
@@ -178,12 +181,14 @@ struct Attn {
     }
   }
 
-  // Weights and sums of one tile of 32 keys, the first of them `key0`.  k_op(h, s), v_op(c): the operands; ef, iv: e + 127 and
-  // 2^-e of this lane's keys of V.  `edge`: some row does not see all keys; lim: the last key that this lane's query sees.
-  template <typename K, typename V>
-  __device__ __forceinline__ void tile(K&& k_op, V&& v_op, const float (&ef)[2][4], const float (&iv)[2][4], int key0, bool edge,
-                                       const int (&lim)[MT], float scale, int grp) {
-    f32x4 s[2][MT];
+  // One tile of 32 keys, the first of them key0, in the parts that a wavefront goes through.  A lane's accumulators hold keys key0
+  // + 16 h + 4 grp + r of query lane & 15; ef, iv: e + 127 and 2^-e of these keys of V; `edge`: some row does not see all keys of the
+  // tile; lim: the last key that this lane's query sees.
+  using Scores = f32x4[2][MT];
+  using Weights = f16x8[MT][PP];
+
+  template <typename K>
+  __device__ __forceinline__ void scores(K&& k_op, Scores& s) const {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -197,28 +202,26 @@ struct Attn {
           for (int p = QP - 1; p >= 0; --p) s[h][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[m][i][p], s[h][m], 0, 0, 0);
       }
     }
-    float x[2][MT][4];                         // log2 of the weights
-    auto hidden = [&](int h, int m, int r) { return edge && key0 + 16 * h + 4 * grp + r > lim[m]; };
-    auto weigh = [&] {
+  }
+
+  // x: log2 of the weights, if no reference moves
+  __device__ __forceinline__ void weigh(const Scores& s, const float (&ef)[2][4], float scale, Scores& x) const {
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) x[h][m][r] = __builtin_fmaf(s[h][m][r], scale, neg_r[m]) + ef[h][r];
-    };
-    auto hide = [&] {
-      if (edge) {
+        for (int r = 0; r < 4; ++r) x[h][m][r] = __builtin_fmaf(s[h][m][r], scale, neg_r[m]) + ef[h][r];
+  }
+  __device__ __forceinline__ void hide(int key0, const int (&lim)[MT], int grp, Scores& x) const {
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[h][m][r] = hidden(h, m, r) ? -__builtin_inff() : x[h][m][r];
-      }
-    };
-    weigh();
-    hide();
+        for (int r = 0; r < 4; ++r) x[h][m][r] = key0 + 16 * h + 4 * grp + r > lim[m] ? -__builtin_inff() : x[h][m][r];
+  }
+  __device__ __forceinline__ bool over(const Scores& x) const {
     float most = -__builtin_inff();
 #pragma unroll
     for (int m = 0; m < MT; ++m)
@@ -226,54 +229,58 @@ struct Attn {
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int r = 0; r < 4; ++r) most = fmaxf(most, x[h][m][r]);
-    if (first || huge || __any(most > kMost)) {
-      // references that hold for this tile too, the sums scaled to them
-      float e_most = E;
+    return first || huge || __any(most > kMost);
+  }
+  // References that hold for this tile too, and the sums scaled to them.
+  __device__ __forceinline__ void move_references(const Scores& s, const float (&ef)[2][4], int key0, bool edge, const int (&lim)[MT],
+                                                  float scale, int grp, Scores& x) {
+    float e_most = E;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) e_most = fmaxf(e_most, ef[h][r]);
+    e_most = over_groups(e_most, [](float a, float b) { return fmaxf(a, b); });
+    const float e_step = exp2_of(E - e_most);
+    E = e_most;
+    float largest = 0.f;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      float y = -__builtin_inff();
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) e_most = fmaxf(e_most, ef[h][r]);
-      e_most = over_groups(e_most, [](float a, float b) { return fmaxf(a, b); });
-      const float e_step = exp2_of(E - e_most);
-      E = e_most;
-      float largest = 0.f;
+        for (int r = 0; r < 4; ++r)
+          y = fmaxf(y, edge && key0 + 16 * h + 4 * grp + r > lim[m] ? -__builtin_inff() : rounded_product(s[h][m][r], scale));
+      y = over_groups(y, [](float a, float b) { return fmaxf(a, b); });
+      // a query that sees none of the tile keeps its reference (0 at first: its sums are 0)
+      const float was = neg_y[m];
+      const bool seen = y > -__builtin_inff();
+      const float now = seen ? (first ? kRef - y : fminf(was, kRef - y)) : was;
+      const float f = first ? 0.f : exp2_of(now - was) * e_step;
+      neg_y[m] = now;
+      neg_r[m] = now - E;
+      l[m] *= f;
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        float y = -__builtin_inff();
+      for (int c = 0; c < DT; ++c) o[m][c] *= f;
+      largest = fmaxf(largest, __builtin_fabsf(now));
+    }
+    huge = __any(largest > kFused);
+    first = false;
+    if (huge) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) y = fmaxf(y, hidden(h, m, r) ? -__builtin_inff() : rounded_product(s[h][m][r], scale));
-        y = over_groups(y, [](float a, float b) { return fmaxf(a, b); });
-        // a query that sees none of the tile keeps its reference (0 at first: its sums are 0)
-        const float was = neg_y[m];
-        const bool seen = y > -__builtin_inff();
-        const float now = seen ? (first ? kRef - y : fminf(was, kRef - y)) : was;
-        const float f = first ? 0.f : exp2_of(now - was) * e_step;
-        neg_y[m] = now;
-        neg_r[m] = now - E;
-        l[m] *= f;
-#pragma unroll
-        for (int c = 0; c < DT; ++c) o[m][c] *= f;
-        largest = fmaxf(largest, __builtin_fabsf(now));
-      }
-      huge = __any(largest > kFused);
-      first = false;
-      if (huge) {
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) x[h][m][r] = (rounded_product(s[h][m][r], scale) + neg_y[m]) + (ef[h][r] - E);
-      } else {
-        weigh();
-      }
-      hide();
+          for (int r = 0; r < 4; ++r) x[h][m][r] = (rounded_product(s[h][m][r], scale) + neg_y[m]) + (ef[h][r] - E);
+    } else {
+      weigh(s, ef, scale, x);
     }
-    f16x8 p[MT][PP];
+    if (edge) hide(key0, lim, grp, x);
+  }
+  __device__ __forceinline__ void weights(const Scores& x, const float (&iv)[2][4], Weights& p) {
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         float w[4];
@@ -294,7 +301,9 @@ struct Attn {
           }
         }
       }
-    }
+  }
+  template <typename V>
+  __device__ __forceinline__ void add_products(V&& v_op, const Weights& p) {
 #pragma unroll
     for (int c = 0; c < DT; ++c) {
       const f16x8 v = v_op(c);
@@ -339,7 +348,16 @@ struct Attn {
 // bytes of the first n of four keys
 __device__ __forceinline__ uint32_t first_bytes(int n) { return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1u; }
 
-// What a workgroup is to do: a tile of M rows of user u's head h from row_first on, keys [key_first, key_last).
+// What a workgroup is to do: a tile of M rows of user u's head h from row_first on, keys [key_first, key_last).  Workgroups are
+// numbered head after head inside
+//   kUsers:  user, tile of rows                             few rows, keys not cut
+//   kKeys:   stretch of keys of all users, tile of rows     few rows: stretches of user u start at its first page's tokens / 2^shift + u
+//   kRows:   tile of rows of all users                      many rows: tiles of user u start at its first row / M + u, the last first
+//                                                           (users of one length: at tiles_each * u)
+//   kBoth:   stretch of a user's keys, tile of all users    many rows of few users, keys cut
+// so that both the stretches and the tiles of users of unlike size follow one another with one place per user left over at most,
+// and a place's user is found from a table that never falls.
+enum class Numbered { kUsers, kKeys, kRows, kBoth };
 struct Work {
   UserSpan us;
   int64_t  item;
@@ -348,46 +366,82 @@ struct Work {
   int      keys;                   // of the whole tile of rows
   bool     partial;                // one of several stretches
 };
-template <int M, bool SPLIT>
-__device__ __forceinline__ bool find_work(const Q8AttnArgs& a, int64_t slot, int qt, int h, Work& w) {
-  int u = (int)slot;
-  w.key_first = 0;
-  auto base = [&](int s) -> int64_t { return (((int64_t)a.b.page_indptr[s] * a.g.S) >> a.chunk_shift) + s; };
-  if constexpr (SPLIT) {
-    u = find_user(a.b.batch, slot, base);
-    const int64_t chunk = slot - base(u);
-    if (chunk < 0 || chunk > (kMostKeys >> a.chunk_shift)) return false;
-    w.key_first = (int)(chunk << a.chunk_shift);
+template <int M>
+__device__ __forceinline__ int64_t first_tile(const Q8AttnArgs& a, int u) {
+  return a.tiles_each > 0 ? (int64_t)u * a.tiles_each : (int64_t)a.b.new_indptr[u] * a.G / M + u;
+}
+__device__ __forceinline__ int64_t first_stretch(const Q8AttnArgs& a, int u) {
+  return (((int64_t)a.b.page_indptr[u] * a.g.S) >> a.chunk_shift) + u;
+}
+template <int M, Numbered N>
+__device__ __forceinline__ bool find_work(const Q8AttnArgs& a, Work& w) {
+  constexpr bool kCut = N == Numbered::kKeys || N == Numbered::kBoth, kAllTiles = N == Numbered::kRows || N == Numbered::kBoth;
+  const uint32_t place = blockIdx.x / (uint32_t)a.g.H;
+  w.h = (int)(blockIdx.x % (uint32_t)a.g.H);
+  w.item = blockIdx.x;
+  int64_t chunk = 0, qt;
+  int u;
+  if constexpr (kAllTiles) {
+    const int64_t tile = N == Numbered::kBoth ? place % (uint32_t)a.slots : place;
+    if constexpr (N == Numbered::kBoth) chunk = place / (uint32_t)a.slots;
+    u = a.tiles_each > 0 ? (int)(tile / a.tiles_each) : find_user(a.b.batch, tile, [&](int s) -> int64_t { return first_tile<M>(a, s); });
+    qt = tile - first_tile<M>(a, u);
+  } else {
+    qt = place % (uint32_t)a.q_tiles;
+    const int64_t slot = place / (uint32_t)a.q_tiles;
+    u = (int)slot;
+    if constexpr (N == Numbered::kKeys) {
+      u = find_user(a.b.batch, slot, [&](int s) -> int64_t { return first_stretch(a, s); });
+      chunk = slot - first_stretch(a, u);
+    }
   }
   w.us = user_span(a.b, a.g.S, u);
-  const int64_t rows = (int64_t)w.us.n * a.G, first = (int64_t)qt * M;
-  if (first >= rows) return false;
-  w.h = h;
+  const int64_t rows = (int64_t)w.us.n * a.G;
+  if (rows <= a.above || rows > a.upto) return false;        // another launch's
+  if constexpr (kAllTiles) qt = (rows + M - 1) / M - 1 - qt;
+  const int64_t first = qt * M;
+  if (first < 0 || first >= rows || chunk < 0 || chunk > (kMostKeys >> a.chunk_shift)) return false;
   w.row_first = (int)first;
   w.row_last = (int)(first + M < rows ? first + M : rows) - 1;
   w.keys = keys_of(w.us, w.row_last, a.G);
+  w.key_first = kCut ? (int)(chunk << a.chunk_shift) : 0;
   if (w.key_first >= w.keys) return false;
-  w.partial = SPLIT && w.keys > (1 << a.chunk_shift);
+  w.partial = kCut && w.keys > (1 << a.chunk_shift);
   w.key_last = w.partial ? min(w.key_first + (1 << a.chunk_shift), w.keys) : w.keys;
-  w.item = (slot * a.q_tiles + qt) * a.g.H + h;
   return true;
 }
 // index of a query row among [total_new][Hq]
 __device__ __forceinline__ int64_t row_at(const Q8AttnArgs& a, const Work& w, int row) {
   return ((int64_t)(w.us.row0 + row / a.G) * a.g.H + w.h) * a.G + row % a.G;
 }
-// Codes and exponents of a 16-token sub-block of the head; those behind the last one, and those of a page that is none, are
-// another's.
+// Where a user's 16-token sub-blocks lie.  The page ids of 64 neighbouring ones are kept in the lanes: a scalar load each would
+// share a counter with the LDS reads, which would then wait for one another.  A sub-block behind the last is the last, a page
+// that is none is page 0.
 template <int D>
-struct SubBlock {
-  const char *k, *v, *ke, *ve;
-  __device__ __forceinline__ SubBlock(const Q8AttnArgs& a, uint32_t id, int64_t head_off, int in_page) {
-    const int64_t page = id < (uint32_t)a.g.num_pages ? id : 0;
-    const char* head = a.g.layer_base + page * a.g.page_bytes + head_off;
-    k = head + in_page * 16 * D;
-    v = k + a.g.S * D;
-    ke = head + 2 * a.g.S * D + in_page * 16;
-    ve = ke + a.g.S;
+struct SubBlocks {
+  const char* head;                // the head's block of page 0
+  const int*  pages;
+  uint32_t    page_bytes, num_pages;
+  int         shift, S, last, have;   // have: the sub-blocks (have, have + 63) are in the lanes
+  int         id;
+  __device__ __forceinline__ SubBlocks(const Q8AttnArgs& a, const Work& w)
+      : head(a.g.layer_base + w.h * q8_head_bytes(a.g.S, D)), pages(a.b.page_indices + w.us.page0), page_bytes((uint32_t)a.g.page_bytes),
+        num_pages((uint32_t)a.g.num_pages), shift(a.g.sub_shift), S(a.g.S), last((w.keys + 15) / 16 - 1), have(-64), id(0) {}
+  // Both sub-blocks of a tile are among the same 64.
+  __device__ __forceinline__ void look_up(int tile) {
+    const int from = 2 * tile & ~63;
+    if (from == have) return;
+    have = from;
+    const uint32_t p = (uint32_t)pages[min(from + (int)(threadIdx.x & 63), last) >> shift];
+    id = (int)(p < num_pages ? p : 0u);
+  }
+  struct At { const char *k, *ke; };
+  __device__ __forceinline__ At at(int sub) const {
+    sub = min(sub, last);
+    const uint32_t page = (uint32_t)__builtin_amdgcn_readlane(id, sub & 63);
+    const char* h = head + (uint64_t)page * page_bytes;
+    const int in_page = sub & ((1 << shift) - 1);
+    return {h + in_page * 16 * D, h + 2 * S * D + in_page * 16};
   }
 };
 // Four dims, from d on, of a row's result or, `partial`, of its stretch.
@@ -408,14 +462,13 @@ __device__ __forceinline__ void store_sums(const Q8AttnArgs& a, const Work& w, i
 }
 
 // Few rows: every wavefront has all of them and every fourth tile of the keys.
-template <int D, int MT, typename T, bool SPLIT>
+template <int D, int MT, typename T, Numbered N>
 __global__ __launch_bounds__(256, D == 128 || MT == 2 ? 2 : 3) void q8_attn_kernel(Q8AttnArgs a) {
   using A = Attn<D, MT, T>;
   constexpr int M = 16 * MT;
   const int lane = threadIdx.x & 63, grp = lane >> 4, wave = uniform_int(threadIdx.x >> 6);
-  const uint32_t rest = blockIdx.x / (uint32_t)a.g.H;
   Work wk;
-  if (!find_work<M, SPLIT>(a, rest / (uint32_t)a.q_tiles, (int)(rest % (uint32_t)a.q_tiles), (int)(blockIdx.x % (uint32_t)a.g.H), wk)) return;
+  if (!find_work<M, N>(a, wk)) return;
   const int all_see = wk.us.prefix + wk.row_first / a.G;     // the last key that every row sees
 
   A c;
@@ -432,22 +485,19 @@ __global__ __launch_bounds__(256, D == 128 || MT == 2 ? 2 : 3) void q8_attn_kern
     typename A::Granule k[2][A::NJ], v[2][A::NJ];
     uint32_t ke[2], ve[2];
   };
-  const int64_t head_off = wk.h * q8_head_bytes(a.g.S, D);
-  const int sub_mask = (1 << a.g.sub_shift) - 1;
-  const int last_sub = (wk.keys + 15) / 16 - 1;
-  const int* pages = a.b.page_indices + wk.us.page0;
+  SubBlocks<D> subs(a, wk);
   auto load = [&](Tile& t, int tile) {
+    subs.look_up(tile);
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      const int sub = min(2 * tile + s, last_sub);
-      const SubBlock<D> at(a, (uint32_t)uniform_int(pages[sub >> a.g.sub_shift]), head_off, sub & sub_mask);
+      const auto at = subs.at(2 * tile + s);
 #pragma unroll
       for (int j = 0; j < A::NJ; ++j) {
         t.k[s][j] = *reinterpret_cast<const typename A::Granule*>(at.k + j * 1024 + lane * A::GB);
-        t.v[s][j] = *reinterpret_cast<const typename A::Granule*>(at.v + j * 1024 + lane * A::GB);
+        t.v[s][j] = *reinterpret_cast<const typename A::Granule*>(at.k + a.g.S * D + j * 1024 + lane * A::GB);
       }
       t.ke[s] = *reinterpret_cast<const uint8_t*>(at.ke + (lane & 15));
-      t.ve[s] = *reinterpret_cast<const uint32_t*>(at.ve + 4 * grp);
+      t.ve[s] = *reinterpret_cast<const uint32_t*>(at.ke + a.g.S + 4 * grp);
     }
   };
   uint32_t nan_seen = 0;
@@ -476,11 +526,17 @@ __global__ __launch_bounds__(256, D == 128 || MT == 2 ? 2 : 3) void q8_attn_kern
 #pragma unroll
       for (int r = 0; r < 4; ++r) { ef[s][r] = exp_of(t.ve[s], r); iv[s][r] = inverse_of(t.ve[s], r); }
     const float ks[2] = {__uint_as_float(t.ke[0] << 23), __uint_as_float(t.ke[1] << 23)};
-    c.tile([&](int h, int i) { return k_operand(t.k[h][i / A::NE][2 * (i % A::NE)], t.k[h][i / A::NE][2 * (i % A::NE) + 1], ks[h]); },
-           [&](int i) {
-             const u32x2 p = v_values(t.v[0][i / A::W][i % A::W]), q = v_values(t.v[1][i / A::W][i % A::W]);
-             return __builtin_bit_cast(f16x8, (u32x4{p[0], p[1], q[0], q[1]}));
-           }, ef, iv, key0, edge, lim, a.scale, grp);
+    typename A::Scores s, x;
+    typename A::Weights p;
+    c.scores([&](int h, int i) { return k_operand(t.k[h][i / A::NE][2 * (i % A::NE)], t.k[h][i / A::NE][2 * (i % A::NE) + 1], ks[h]); }, s);
+    c.weigh(s, ef, a.scale, x);
+    if (edge) c.hide(key0, lim, grp, x);
+    if (c.over(x)) c.move_references(s, ef, key0, edge, lim, a.scale, grp, x);
+    c.weights(x, iv, p);
+    c.add_products([&](int i) {
+      const u32x2 lo = v_values(t.v[0][i / A::W][i % A::W]), hi = v_values(t.v[1][i / A::W][i % A::W]);
+      return __builtin_bit_cast(f16x8, (u32x4{lo[0], lo[1], hi[0], hi[1]}));
+    }, p);
   };
   const int tile_end = (wk.key_last + 31) / 32;
   int tile = wk.key_first / 32 + wave;
@@ -576,8 +632,9 @@ __global__ __launch_bounds__(256, D == 128 || MT == 2 ? 2 : 3) void q8_attn_kern
 }
 
 // Many rows: the wavefronts have 16 MT rows each and go through the keys together.  A tile of 32 keys is converted to operands
-// once, a quarter by each wavefront, into one of two stages in LDS, while the other is multiplied from.
-template <int D, int MT, typename T, bool SPLIT>
+// once, a quarter by each wavefront, into one of two stages in LDS, while the other is multiplied from.  Workgroups go to the 8
+// XCDs in turn, so that with the heads counted first the tiles of a (user, head) meet its keys in one XCD's L2 (8 heads), or two's.
+template <int D, int MT, typename T, Numbered N>
 __global__ __launch_bounds__(256, 2) void q8_attn_wide_kernel(Q8AttnArgs a) {
   using A = Attn<D, MT, T>;
   constexpr int M = 64 * MT;
@@ -589,13 +646,8 @@ __global__ __launch_bounds__(256, 2) void q8_attn_wide_kernel(Q8AttnArgs a) {
   __shared__ Stage stage[2];
   __shared__ int nan_seen[2];
   const int lane = threadIdx.x & 63, grp = lane >> 4, wave = uniform_int(threadIdx.x >> 6);
-  // Workgroups go to the 8 XCDs in turn; the tiles of one (user, head) share its keys in one XCD's L2: eight pairs at a time, a pair
-  // per XCD, the longest tiles first.
-  const uint32_t pairs = (uint32_t)(a.slots * a.g.H), per8 = 8u * (uint32_t)a.q_tiles;
-  const uint32_t eight = blockIdx.x / per8, in8 = blockIdx.x % per8, left = min(8u, pairs - 8u * eight);
-  const uint32_t pair = 8u * eight + in8 % left;
   Work wk;
-  if (!find_work<M, SPLIT>(a, pair / (uint32_t)a.g.H, a.q_tiles - 1 - (int)(in8 / left), (int)(pair % (uint32_t)a.g.H), wk)) return;
+  if (!find_work<M, N>(a, wk)) return;
 
   A c;
   c.start();
@@ -613,26 +665,27 @@ __global__ __launch_bounds__(256, 2) void q8_attn_wide_kernel(Q8AttnArgs a) {
   // this wavefront's part of a tile: K (0, 1) or V (2, 3) of one of the two sub-blocks
   const int my_sub = wave & 1;
   const bool is_v = wave >= 2;
-  const int64_t head_off = wk.h * q8_head_bytes(a.g.S, D);
-  const int sub_mask = (1 << a.g.sub_shift) - 1;
-  const int last_sub = (wk.keys + 15) / 16 - 1;
-  const int* pages = a.b.page_indices + wk.us.page0;
+  SubBlocks<D> subs(a, wk);
   struct Raw {
     typename A::Granule g[A::NJ];
     uint32_t e;
   };
-  auto sub_of = [&](int tile) { return min(2 * tile + my_sub, last_sub); };
-  auto load = [&](Raw& r, int tile, int id) {
-    const SubBlock<D> at(a, (uint32_t)id, head_off, sub_of(tile) & sub_mask);
+  const int codes_at = (is_v ? a.g.S * D : 0) + lane * A::GB, exps_at = (is_v ? a.g.S : 0) + (lane & 15);
+  auto load = [&](Raw& r, int tile) {
+    subs.look_up(tile);
+    const auto at = subs.at(2 * tile + my_sub);
 #pragma unroll
-    for (int j = 0; j < A::NJ; ++j) r.g[j] = *reinterpret_cast<const typename A::Granule*>((is_v ? at.v : at.k) + j * 1024 + lane * A::GB);
-    r.e = *reinterpret_cast<const uint8_t*>((is_v ? at.ve : at.ke) + (lane & 15));
+    for (int j = 0; j < A::NJ; ++j) r.g[j] = *reinterpret_cast<const typename A::Granule*>(at.k + j * 1024 + codes_at);
+    r.e = *reinterpret_cast<const uint8_t*>(at.ke + exps_at);
   };
-  auto page_of = [&](int tile) { return uniform_int(pages[sub_of(tile) >> a.g.sub_shift]); };
-  auto convert = [&](Raw& r, int tile, Stage& st) {
+  const int tile_end = (wk.key_last + 31) / 32, tile_first = wk.key_first / 32;
+  auto convert = [&](Raw& r, int tile) {
+    const int key0 = tile * 32 + 16 * my_sub;
+    Stage& st = stage[(tile - tile_first) & 1];
     if (is_v) {
-      const int key0 = tile * 32 + 16 * my_sub;
+      uint32_t e = r.e;
       if (tile * 32 + 31 > all_rows_see) {
+        if (key0 + (lane & 15) >= wk.key_last) e = (uint32_t)kNoExp;
         const uint32_t keep = first_bytes(wk.key_last - (key0 + 4 * grp));
         uint32_t any = 0;
 #pragma unroll
@@ -644,51 +697,58 @@ __global__ __launch_bounds__(256, 2) void q8_attn_wide_kernel(Q8AttnArgs a) {
             any |= nan;
           }
         if (any) nan_seen[my_sub] = 1;
-        r.e = key0 + (lane & 15) < wk.key_last ? r.e : (uint32_t)kNoExp;
       }
 #pragma unroll
       for (int j = 0; j < A::NJ; ++j)
 #pragma unroll
         for (int w = 0; w < A::W; ++w) reinterpret_cast<u32x2*>(&st.v[j * A::W + w][lane])[my_sub] = v_values(r.g[j][w]);
       if (lane < 16) {
-        st.ef[my_sub][lane] = (float)r.e;
-        st.iv[my_sub][lane] = inverse_of(r.e, 0);
+        st.ef[my_sub][lane] = (float)e;
+        st.iv[my_sub][lane] = inverse_of(e, 0);
       }
     } else {
       const float scale = __uint_as_float(r.e << 23);
 #pragma unroll
       for (int i = 0; i < A::KS; ++i)
-        st.k[my_sub][i][lane] = __builtin_bit_cast(u32x4, k_operand(r.g[i / A::NE][2 * (i % A::NE)], r.g[i / A::NE][2 * (i % A::NE) + 1], scale));
+        st.k[my_sub][i][lane] =
+            __builtin_bit_cast(u32x4, k_operand(r.g[i / A::NE][2 * (i % A::NE)], r.g[i / A::NE][2 * (i % A::NE) + 1], scale));
     }
   };
-  const int tile_end = (wk.key_last + 31) / 32, tile_first = wk.key_first / 32;
+  auto four_of = [&](const float (&from)[2][16], float (&to)[2][4]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const f32x4 e = *reinterpret_cast<const f32x4*>(&from[h][4 * grp]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) to[h][r] = e[r];
+    }
+  };
   if (threadIdx.x < 2) nan_seen[threadIdx.x] = 0;
   __syncthreads();
   Raw raw;
-  load(raw, tile_first, page_of(tile_first));
-  convert(raw, tile_first, stage[0]);
-  load(raw, tile_first + 1, page_of(tile_first + 1));
-  int id = page_of(tile_first + 2);
+  load(raw, tile_first);
+  convert(raw, tile_first);
+  load(raw, tile_first + 1);
   __syncthreads();
   for (int tile = tile_first; tile < tile_end; ++tile) {
-    Stage& st = stage[(tile - tile_first) & 1];
+    const Stage& st = stage[(tile - tile_first) & 1];
     if (tile + 1 < tile_end) {
-      convert(raw, tile + 1, stage[(tile + 1 - tile_first) & 1]);
-      load(raw, tile + 2, id);
-      id = page_of(tile + 3);
+      convert(raw, tile + 1);
+      load(raw, tile + 2);
     }
     const int key0 = tile * 32;
     if (key0 <= some_see) {
       const bool edge = key0 + 31 > all_see;
+      typename A::Scores s, x;
+      typename A::Weights p;
       float ef[2][4], iv[2][4];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const f32x4 e = *reinterpret_cast<const f32x4*>(&st.ef[h][4 * grp]), i = *reinterpret_cast<const f32x4*>(&st.iv[h][4 * grp]);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) { ef[h][r] = e[r]; iv[h][r] = i[r]; }
-      }
-      c.tile([&](int h, int i) { return __builtin_bit_cast(bf16x8, st.k[h][i][lane]); },
-             [&](int i) { return __builtin_bit_cast(f16x8, st.v[i][lane]); }, ef, iv, key0, edge, lim, a.scale, grp);
+      four_of(st.ef, ef);
+      four_of(st.iv, iv);
+      c.scores([&](int h, int i) { return __builtin_bit_cast(bf16x8, st.k[h][i][lane]); }, s);
+      c.weigh(s, ef, a.scale, x);
+      if (edge) c.hide(key0, lim, grp, x);
+      if (c.over(x)) c.move_references(s, ef, key0, edge, lim, a.scale, grp, x);
+      c.weights(x, iv, p);
+      c.add_products([&](int i) { return __builtin_bit_cast(f16x8, st.v[i][lane]); }, p);
     }
     __syncthreads();
   }
@@ -696,14 +756,14 @@ __global__ __launch_bounds__(256, 2) void q8_attn_wide_kernel(Q8AttnArgs a) {
     for (int again = tile_first; again < tile_end; ++again)
       if (again * 32 + 31 > all_rows_see) {
         typename A::Granule v[2][A::NJ];
+        subs.look_up(again);
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-          const int sub = min(2 * again + s, last_sub);
-          const SubBlock<D> at(a, (uint32_t)uniform_int(pages[sub >> a.g.sub_shift]), head_off, sub & sub_mask);
+          const auto at = subs.at(2 * again + s);
           const uint32_t keep = first_bytes(wk.key_last - (again * 32 + 16 * s + 4 * grp));
 #pragma unroll
           for (int j = 0; j < A::NJ; ++j) {
-            v[s][j] = *reinterpret_cast<const typename A::Granule*>(at.v + j * 1024 + lane * A::GB);
+            v[s][j] = *reinterpret_cast<const typename A::Granule*>(at.k + a.g.S * D + j * 1024 + lane * A::GB);
 #pragma unroll
             for (int w = 0; w < A::W; ++w) v[s][j][w] &= keep;
           }
@@ -723,13 +783,17 @@ __global__ __launch_bounds__(256, 2) void q8_attn_wide_kernel(Q8AttnArgs a) {
   }
 }
 
-// Joins the stretches of a row's keys, in their order: one wavefront per (token, query head).
-template <int D, typename T>
-__global__ __launch_bounds__(256) void q8_join_kernel(Q8AttnArgs a, int tile_rows) {
-  const int lane = threadIdx.x & 63;
+// Joins the stretches of a row's keys, in an order that only their number decides: one wavefront or four per (token, query head),
+// D / 4 lanes to a stretch, so that 2 to 32 of them are read at once and a long history's hundreds take no chain of round trips.
+template <int D, typename T, int M, Numbered N, int WAVES>
+__global__ __launch_bounds__(256) void q8_join_kernel(Q8AttnArgs a) {
+  constexpr int L = D / 4, P = 64 / L;                       // lanes of a stretch, stretches of a wavefront
+  __shared__ float most[4], xl[4];
+  __shared__ f32x4 xo[4][L];
+  const int lane = threadIdx.x & 63, wave = uniform_int(threadIdx.x >> 6);
   const int Hq = a.g.H * a.G;
-  const int64_t unit = (int64_t)blockIdx.x * 4 + uniform_int(threadIdx.x >> 6);
-  const int token = (int)(unit / Hq), hq = (int)(unit % Hq);
+  const uint32_t unit = WAVES == 4 ? blockIdx.x : blockIdx.x * 4 + wave;
+  const int token = (int)(unit / (uint32_t)Hq), hq = (int)(unit % (uint32_t)Hq);
   if (token >= a.b.total_new) return;
   const int u = find_user(a.b.batch, token, [&](int s) -> int64_t { return a.b.new_indptr[s]; });
   const UserSpan us = user_span(a.b, a.g.S, u);
@@ -737,104 +801,219 @@ __global__ __launch_bounds__(256) void q8_join_kernel(Q8AttnArgs a, int tile_row
   if (i < 0 || i >= us.n) return;
   const int h = hq / a.G;
   const int64_t row = (int64_t)i * a.G + hq % a.G, rows = (int64_t)us.n * a.G;
-  const int qt = (int)(row / tile_rows);
-  if (qt >= a.q_tiles) return;
-  const int64_t tile_end = (int64_t)(qt + 1) * tile_rows;
-  const int keys = keys_of(us, (int)((tile_end < rows ? tile_end : rows) - 1), a.G);
+  if (rows <= a.above || rows > a.upto) return;
+  const int64_t qt = row / M, last = (qt + 1) * M < rows ? (qt + 1) * M : rows;
+  const int keys = keys_of(us, (int)last - 1, a.G);
   const int chunks = (int)(((int64_t)keys + (1ll << a.chunk_shift) - 1) >> a.chunk_shift);
   if (chunks <= 1) return;
-  const int64_t slot = (((int64_t)a.b.page_indptr[u] * a.g.S) >> a.chunk_shift) + u;
-  if (slot < 0 || slot + chunks > a.slots) return;
-  const int64_t step = (int64_t)a.q_tiles * a.g.H * a.part_rows;                  // rows from a stretch to the next
-  const int64_t at = (slot * a.q_tiles + qt) * a.g.H * a.part_rows + (int64_t)h * a.part_rows + row % tile_rows;
+  // the first stretch's place, and places from one to the next
+  int64_t place, next;
+  if constexpr (N == Numbered::kKeys) {
+    const int64_t slot = first_stretch(a, u);
+    if (qt >= a.q_tiles || slot < 0 || slot + chunks > a.slots) return;
+    place = slot * a.q_tiles + qt;
+    next = a.q_tiles;
+  } else {
+    place = first_tile<M>(a, u) + (rows + M - 1) / M - 1 - qt;
+    next = a.slots;
+    if (place < 0 || place >= a.slots || chunks > a.q_tiles) return;
+  }
+  const int64_t step = next * a.g.H * a.part_rows;           // rows from a stretch to the next
+  const int64_t at = (place * a.g.H + h) * a.part_rows + row % M;
   float y = -__builtin_inff();
-  for (int k = lane; k < chunks; k += 64) y = fmaxf(y, a.part_ml[(at + k * step) * 2]);
+  for (int k = WAVES == 4 ? threadIdx.x : lane; k < chunks; k += 64 * WAVES) y = fmaxf(y, a.part_ml[(at + k * step) * 2]);
 #pragma unroll
   for (int s = 1; s < 64; s <<= 1) y = fmaxf(y, __shfl_xor(y, s));
+  if constexpr (WAVES == 4) {
+    if (lane == 0) most[wave] = y;
+    __syncthreads();
+    y = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+  }
   const float ref = y > -__builtin_inff() ? y : 0.f;
-  constexpr int PER = D >= 64 ? D / 64 : 1;
-  const bool mine = lane * PER < D;
-  float acc[PER] = {}, l = 0.f;
-  for (int k = 0; k < chunks; ++k) {
+  f32x4 acc{0.f, 0.f, 0.f, 0.f};
+  float l = 0.f;
+#pragma unroll 4
+  for (int k = (WAVES == 4 ? wave * P : 0) + lane / L; k < chunks; k += WAVES * P) {
     const f32x2 ml = *reinterpret_cast<const f32x2*>(a.part_ml + (at + k * step) * 2);
+    const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + (at + k * step) * D + 4 * (lane % L));
     const float f = exp2_of(ml[0] - ref);
     l = __builtin_fmaf(ml[1], f, l);
-    if (mine) {
-#pragma unroll
-      for (int j = 0; j < PER; ++j) acc[j] = __builtin_fmaf(a.part_o[(at + k * step) * D + lane * PER + j], f, acc[j]);
-    }
+    acc += v * f;
   }
-  if (!mine) return;
-  const int64_t dst = ((int64_t)token * Hq + hq) * D + lane * PER;
 #pragma unroll
-  for (int j = 0; j < PER; ++j) {
-    const float v = acc[j] / l;
-    if constexpr (std::is_same<T, float>::value) *reinterpret_cast<float*>(a.out + (dst + j) * 4) = v;
-    else *reinterpret_cast<__bf16*>(a.out + (dst + j) * 2) = (__bf16)v;
+  for (int s = L; s < 64; s <<= 1) {
+    l += __shfl_xor(l, s);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] += __shfl_xor(acc[j], s);
+  }
+  if constexpr (WAVES == 4) {
+    if (lane < L) xo[wave][lane] = acc;
+    if (lane == 0) xl[wave] = l;
+    __syncthreads();
+    if (wave > 0) return;
+    acc = (xo[0][lane % L] + xo[1][lane % L]) + (xo[2][lane % L] + xo[3][lane % L]);
+    l = (xl[0] + xl[1]) + (xl[2] + xl[3]);
+  }
+  if (lane >= L) return;
+  const f32x4 v = acc * (1.f / l);
+  const int64_t dst = ((int64_t)token * Hq + hq) * D + 4 * lane;
+  if constexpr (std::is_same<T, float>::value) {
+    *reinterpret_cast<f32x4*>(a.out + dst * 4) = v;
+  } else {
+    const bf16x2 lo = __builtin_convertvector((f32x2{v[0], v[1]}), bf16x2), hi = __builtin_convertvector((f32x2{v[2], v[3]}), bf16x2);
+    *reinterpret_cast<u32x2*>(a.out + dst * 2) = u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
   }
 }
 
 }  // namespace
 
+constexpr int kWideRows = 128, kFewRows = 64;
+
 Q8AttnPlan plan_q8_attention(const Q8Geom& g, int32_t num_q_heads, const BatchDev& b) {
   Q8AttnPlan p{};
   const int64_t G = num_q_heads / g.H, rows = G * b.max_new;
-  p.wide = rows >= 128;
-  p.rows = p.wide ? 128 : rows > 16 ? 32 : 16;
-  p.q_tiles = (int)((rows + p.rows - 1) / p.rows);
-  p.chunk_shift = 31;
-  p.part_rows = (int)(rows < p.rows ? rows : p.rows);
-  p.slots = b.batch;
   p.too_large = rows >= (1ll << 30) || b.max_total_len > kMostKeys;
   if (p.too_large || b.total_new <= 0 || b.batch <= 0) return p;
-  const int64_t pairs = (int64_t)p.q_tiles * g.H;
   const int64_t held = (int64_t)b.total_pages * g.S, most = (int64_t)b.batch * b.max_total_len;
   const int64_t keys = held < most ? held : most;
-  if (b.batch * pairs < 4096 && b.max_total_len > 256) {
-    int shift = 8;
-    while (shift < 30 && (keys >> shift) * pairs > 2048) ++shift;
-    if ((1ll << shift) < b.max_total_len) {
-      p.chunk_shift = shift;
-      p.slots = (held >> shift) + b.batch;
+  auto finish = [&](Q8AttnLaunch& l, int64_t places) {
+    l.on = true;
+    l.items = places * g.H;
+    p.too_large |= l.items >= (1ll << 31);
+    if (l.chunk_shift < 31) {
+      const int64_t bytes = (l.items * l.part_rows * (g.D + 2) * (int64_t)sizeof(float) + 255) / 256 * 256;
+      if (bytes > p.ws_bytes) p.ws_bytes = bytes;
     }
+  };
+  const bool wide = rows >= kWideRows;
+  if (wide) {
+    // Users of many rows.  Where their tiles fill the chip (two workgroups on each of 256 CUs) they are not cut; where they do not,
+    // and the longest is not short, or a tile sees so many keys that a stretch's 128 rows (66 KB written and read again at
+    // head_dim 128) are little beside them, the keys are.  us a call, cut into stretches of 256 and more / uncut: 8 users of
+    // 1588-3176 x 3 heads of 64, fp32 134 / 108; 4 of 284-2279 x 3 (4 query heads each) of 128 156 / 107; 1 of 837 x 5 of 128
+    // 41 / 23; of 512 and more / uncut: 2 of 427-3420 x 4 of 32 32 / 42; of 2048 and more / uncut: 28 users of 10-20 tokens behind
+    // 8-14 K x 8 (8 query heads each) of 64 230 / 356, 32 of 16-32 behind 4-16 K x 8 (4) of 128 296 / 496.
+    Q8AttnLaunch& l = p.wide;
+    l.rows = l.part_rows = kWideRows;
+    l.above = 0;
+    l.upto = INT32_MAX;
+    l.chunk_shift = 31;
+    l.q_tiles = 1;
+    if (b.total_new == (int64_t)b.batch * b.max_new) {
+      l.tiles_each = (int)((rows + kWideRows - 1) / kWideRows);
+      l.slots = (int64_t)b.batch * l.tiles_each;
+    } else {
+      l.slots = (int64_t)b.total_new * G / kWideRows + b.batch;
+    }
+    const int64_t tiles = l.slots * g.H, seen = (held - b.total_new / 2) / b.batch;   // keys of a tile, about
+    const bool few_tiles = tiles < 384 && b.max_total_len > 1024;
+    if (few_tiles || (tiles < 2048 && seen >= 4096)) {
+      int shift = few_tiles ? 9 : 11;
+      while (shift < 30 && (few_tiles ? ((int64_t)b.max_total_len - 1) >> shift : seen >> shift) * tiles > (few_tiles ? 1024 : 2048)) ++shift;
+      if ((1ll << shift) < b.max_total_len) {
+        l.chunk_shift = shift;
+        l.q_tiles = (int)((((int64_t)b.max_total_len - 1) >> shift) + 1);   // stretches of the longest user
+      }
+    }
+    finish(l, l.slots * l.q_tiles);
   }
-  p.items = p.slots * pairs;
-  p.too_large = p.items >= (1ll << 31);
-  if (p.chunk_shift < 31) p.ws_bytes = (p.items * p.part_rows * (g.D + 2) * (int64_t)sizeof(float) + 255) / 256 * 256;
+  // Users of few rows beside them, unless the sizes leave none: a launch of their own, whose wavefronts share out the keys and
+  // not the rows.  It costs 4 us, which short histories do not repay.
+  const int64_t least = b.total_new - (b.batch - 1ll) * b.max_new;         // of a user, if all others have the most
+  if (!wide || (least * G <= kFewRows && b.max_total_len > 1024)) {
+    Q8AttnLaunch& l = p.few;
+    const int64_t most_rows = wide ? kFewRows : rows;
+    if (wide) p.wide.above = kFewRows;
+    l.above = 0;
+    l.upto = wide ? kFewRows : INT32_MAX;
+    l.rows = most_rows > 16 ? 32 : 16;
+    l.part_rows = (int)(most_rows < l.rows ? most_rows : l.rows);
+    l.q_tiles = (int)((most_rows + l.rows - 1) / l.rows);
+    l.chunk_shift = 31;
+    l.slots = b.batch;
+    // About 2048 workgroups, each with at least 256 keys.  us a call with 1024, 2048, 4096 workgroups: 32 users x 10 K keys x 8
+    // heads of 128 144, 140, 142; 32 rows each 166, 164, 172; 64 x 1.5 K x 8 of 64 28.8, 27.8, 31.4; with 128 keys and more 60 K keys
+    // x 4 15.3 where 12.4.
+    const int64_t pairs = (int64_t)l.q_tiles * g.H;
+    if (b.batch * pairs < 4096 && b.max_total_len > 256) {
+      int shift = 8;
+      while (shift < 30 && (keys >> shift) * pairs > 2048) ++shift;
+      if ((1ll << shift) < b.max_total_len) {
+        l.chunk_shift = shift;
+        l.slots = (held >> shift) + b.batch;
+      }
+    }
+    finish(l, l.slots * l.q_tiles);
+  }
   return p;
 }
 
+template <int D, typename T, int M, Numbered N>
+static void launch_join(const Q8AttnArgs& a, hipStream_t stream) {
+  // By the stretches of the longest user: a chain of many loads is shared by four wavefronts, a chain of a few too where the
+  // rows do not fill the chip.  us a call, one wavefront / four: 70 K keys x 4 heads, 274 stretches 28.7 / 12.6; 55 users' single
+  // tokens, 11 stretches, 165 rows 12.6 / 12.0; 2 users' 3 K tokens, 13 stretches, 15 K rows 31 / 50.
+  const int64_t units = (int64_t)a.b.total_new * a.g.H * a.G;
+  if ((a.b.max_total_len >> a.chunk_shift) >= (units <= 512 ? 8 : 32)) q8_join_kernel<D, T, M, N, 4><<<dim3((unsigned)units), dim3(256), 0, stream>>>(a);
+  else q8_join_kernel<D, T, M, N, 1><<<dim3((unsigned)((units + 3) / 4)), dim3(256), 0, stream>>>(a);
+}
+
 template <int D, typename T>
-static hipError_t launch(const Q8AttnArgs& a, const Q8AttnPlan& p, hipStream_t stream) {
-  const dim3 grid((unsigned)p.items), block(256);
-  const bool split = p.chunk_shift < 31;
-  if (p.wide) {
-    if (split) q8_attn_wide_kernel<D, 2, T, true><<<grid, block, 0, stream>>>(a);
-    else q8_attn_wide_kernel<D, 2, T, false><<<grid, block, 0, stream>>>(a);
-  } else if (p.rows == 16) {
-    if (split) q8_attn_kernel<D, 1, T, true><<<grid, block, 0, stream>>>(a);
-    else q8_attn_kernel<D, 1, T, false><<<grid, block, 0, stream>>>(a);
-  } else {
-    if (split) q8_attn_kernel<D, 2, T, true><<<grid, block, 0, stream>>>(a);
-    else q8_attn_kernel<D, 2, T, false><<<grid, block, 0, stream>>>(a);
-  }
-  if (split) {
+static hipError_t launch(Q8AttnArgs a, const Q8AttnPlan& p, void* workspace, hipStream_t stream) {
+  const dim3 block(256);
+  auto take = [&](const Q8AttnLaunch& l) {
+    a.above = l.above;
+    a.upto = l.upto;
+    a.q_tiles = l.q_tiles;
+    a.tiles_each = l.tiles_each;
+    a.chunk_shift = l.chunk_shift;
+    a.part_rows = l.part_rows;
+    a.slots = l.slots;
+    a.part_o = (float*)workspace;
+    a.part_ml = (float*)workspace + l.items * l.part_rows * D;
+    return dim3((unsigned)l.items);
+  };
+  if (p.wide.on) {
+    const dim3 grid = take(p.wide);
+    if (a.chunk_shift < 31) {
+      q8_attn_wide_kernel<D, 2, T, Numbered::kBoth><<<grid, block, 0, stream>>>(a);
+      launch_join<D, T, kWideRows, Numbered::kBoth>(a, stream);
+    } else {
+      q8_attn_wide_kernel<D, 2, T, Numbered::kRows><<<grid, block, 0, stream>>>(a);
+    }
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    const int64_t units = (int64_t)a.b.total_new * a.g.H * a.G;
-    q8_join_kernel<D, T><<<dim3((unsigned)((units + 3) / 4)), block, 0, stream>>>(a, p.rows);
+    if (e != hipSuccess || !p.few.on) return e;
+  }
+  const dim3 grid = take(p.few);
+  if (p.few.rows == 16) {
+    if (a.chunk_shift < 31) {
+      q8_attn_kernel<D, 1, T, Numbered::kKeys><<<grid, block, 0, stream>>>(a);
+      launch_join<D, T, 16, Numbered::kKeys>(a, stream);
+    } else {
+      q8_attn_kernel<D, 1, T, Numbered::kUsers><<<grid, block, 0, stream>>>(a);
+    }
+  } else if (a.chunk_shift < 31) {
+    q8_attn_kernel<D, 2, T, Numbered::kKeys><<<grid, block, 0, stream>>>(a);
+    launch_join<D, T, 32, Numbered::kKeys>(a, stream);
+  } else {
+    q8_attn_kernel<D, 2, T, Numbered::kUsers><<<grid, block, 0, stream>>>(a);
   }
   return hipGetLastError();
 }
 
 hipError_t launch_q8_attn(const Q8Geom& g, const Q8AttnPlan& plan, bool f32, int32_t num_q_heads, const void* q, void* out,
                           const BatchDev& b, float sm_scale, void* workspace, hipStream_t stream) {
-  Q8AttnArgs a{g, (const char*)q, (char*)out, b, sm_scale * kLog2e, num_q_heads / g.H, plan.q_tiles, plan.chunk_shift, plan.part_rows,
-               plan.slots, (float*)workspace, (float*)workspace + plan.items * plan.part_rows * g.D};
+  Q8AttnArgs a{};
+  a.g = g;
+  a.q = (const char*)q;
+  a.out = (char*)out;
+  a.b = b;
+  a.scale = sm_scale * kLog2e;
+  a.G = num_q_heads / g.H;
   switch (g.D) {
-    case 32: return f32 ? launch<32, float>(a, plan, stream) : launch<32, uint16_t>(a, plan, stream);
-    case 64: return f32 ? launch<64, float>(a, plan, stream) : launch<64, uint16_t>(a, plan, stream);
-    default: return f32 ? launch<128, float>(a, plan, stream) : launch<128, uint16_t>(a, plan, stream);
+    case 32: return f32 ? launch<32, float>(a, plan, workspace, stream) : launch<32, uint16_t>(a, plan, workspace, stream);
+    case 64: return f32 ? launch<64, float>(a, plan, workspace, stream) : launch<64, uint16_t>(a, plan, workspace, stream);
+    default: return f32 ? launch<128, float>(a, plan, workspace, stream) : launch<128, uint16_t>(a, plan, workspace, stream);
   }
 }
 

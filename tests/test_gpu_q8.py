@@ -263,6 +263,18 @@ def test_segments_of_many_tiles(H, G, D, S, new, dtype):
     attend(23, H, G, D, S, [0, 100, 40, 333], new, dtype)
 
 
+@pytest.mark.parametrize("H,G,D,S,prefix,new", [
+    (2, 1, 64, 16, [3000, 0, 500, 0, 1200, 7, 900], [1, 300, 20, 0, 2, 64, 65]),     # both kinds cut and joined
+    (3, 2, 128, 32, [40, 0, 500, 0, 100], [1, 150, 32, 33, 200]),                    # neither
+    (1, 4, 32, 16, [700, 1500], [200, 1]),
+    (2, 2, 64, 64, [10, 300], [140, 140]),                                           # no user of few rows: one kernel
+    (2, 1, 128, 16, [2000], [129]),
+])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_users_of_few_and_of_many_rows_in_one_call(H, G, D, S, prefix, new, dtype):
+    attend(36, H, G, D, S, prefix, new, dtype)
+
+
 def test_tiles_of_rows_and_stretches_of_keys_at_once():
     # some rows of a tile see none of its last stretch's keys
     s, _, _ = attend(24, 1, 2, 64, 16, [1000, 240], [70, 40], "bf16")
