@@ -773,7 +773,7 @@ int64_t mts_attn_q8_workspace_bytes(const mts_cache_desc* cache, int32_t num_q_h
   if ((st = check_q8_cache(cache, 0, false, &g)) != MTS_OK) return st;
   if ((st = check_q_heads(g, num_q_heads)) != MTS_OK) return st;
   if ((st = check_meta(meta, true, false, &b)) != MTS_OK) return st;
-  const mts::Q8AttnPlan p = mts::plan_q8_attention(g, num_q_heads, b);
+  const mts::Q8AttnPlan p = mts::plan_q8_attention(g, num_q_heads, b, cache->num_layers);
   if (p.too_large) return too_large_q8(b);
   return p.ws_bytes;
 }
@@ -793,7 +793,7 @@ int32_t mts_attn_incremental_q8(const mts_cache_desc* cache, int32_t layer, int3
   if (b.batch == 0 || b.total_new == 0) return MTS_OK;
   if (!q || !out) return fail(MTS_ERR_INVALID_ARG, "q / out is NULL");
   if (!aligned(q, 16) || !aligned(out, 16)) return fail(MTS_ERR_INVALID_ARG, "q / out is not 16-byte aligned");
-  const mts::Q8AttnPlan plan = mts::plan_q8_attention(g, num_q_heads, b);
+  const mts::Q8AttnPlan plan = mts::plan_q8_attention(g, num_q_heads, b, cache->num_layers);
   if (plan.too_large) return too_large_q8(b);
   if (plan.ws_bytes > 0) {
     if (!workspace) return fail(MTS_ERR_WORKSPACE, "workspace is NULL but %lld bytes are needed", (long long)plan.ws_bytes);

@@ -163,9 +163,10 @@ struct Q8AttnLaunch {
 struct Q8AttnPlan {
   Q8AttnLaunch wide, few;    // one after the other, in the same workspace
   int64_t      ws_bytes;
+  bool         past_caches;  // few rows: K and V are loaded past the caches' retention
   bool         too_large;
 };
-Q8AttnPlan plan_q8_attention(const Q8Geom& g, int32_t num_q_heads, const BatchDev& b);
+Q8AttnPlan plan_q8_attention(const Q8Geom& g, int32_t num_q_heads, const BatchDev& b, int32_t layers);
 hipError_t launch_q8_attn(const Q8Geom& g, const Q8AttnPlan& plan, bool f32, int32_t num_q_heads, const void* q, void* out,
                           const BatchDev& b, float sm_scale, void* workspace, hipStream_t stream);
 

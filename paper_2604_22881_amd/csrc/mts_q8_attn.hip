@@ -444,6 +444,11 @@ struct SubBlocks {
     return {h + in_page * 16 * D, h + 2 * S * D + in_page * 16};
   }
 };
+template <bool PAST, typename Granule>
+__device__ __forceinline__ Granule load_granule(const char* p) {
+  if constexpr (PAST) return __builtin_nontemporal_load(reinterpret_cast<const Granule*>(p));
+  else return *reinterpret_cast<const Granule*>(p);
+}
 // Four dims, from d on, of a row's result or, `partial`, of its stretch.
 template <int D, typename T>
 __device__ __forceinline__ void store_sums(const Q8AttnArgs& a, const Work& w, int row, int d, f32x4 v, float inv) {
@@ -461,9 +466,10 @@ __device__ __forceinline__ void store_sums(const Q8AttnArgs& a, const Work& w, i
   }
 }
 
-// Few rows: every wavefront has all of them and every fourth tile of the keys.
-template <int D, int MT, typename T, Numbered N>
-__global__ __launch_bounds__(256, D == 128 || MT == 2 ? 2 : 3) void q8_attn_kernel(Q8AttnArgs a) {
+// Few rows: every wavefront has all of them and every fourth tile of the keys.  PAST: K and V past the caches' retention, where a
+// call reads nothing of them twice (kv_past_caches): 32 users x 10 K keys x 8 heads of 128 141 -> 130 us.
+template <int D, int MT, typename T, Numbered N, bool PAST>
+__global__ __launch_bounds__(256, (MT == 2 || (D == 128 && std::is_same<T, float>::value)) ? 2 : 3) void q8_attn_kernel(Q8AttnArgs a) {
   using A = Attn<D, MT, T>;
   constexpr int M = 16 * MT;
   const int lane = threadIdx.x & 63, grp = lane >> 4, wave = uniform_int(threadIdx.x >> 6);
@@ -486,24 +492,40 @@ __global__ __launch_bounds__(256, D == 128 || MT == 2 ? 2 : 3) void q8_attn_kern
     uint32_t ke[2], ve[2];
   };
   SubBlocks<D> subs(a, wk);
-  auto load = [&](Tile& t, int tile) {
-    subs.look_up(tile);
+  // Of 128 dims one tile is in registers: K of the next is asked for when its operands have been made, V when its own have (two
+  // tiles, as of fewer dims, take 34 registers more and a third workgroup from a CU; of 64 dims one tile is 4 to 6 % slower).
+  constexpr bool kTwo = D <= 64;
+  auto load_k = [&](Tile& t, int tile) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       const auto at = subs.at(2 * tile + s);
 #pragma unroll
-      for (int j = 0; j < A::NJ; ++j) {
-        t.k[s][j] = *reinterpret_cast<const typename A::Granule*>(at.k + j * 1024 + lane * A::GB);
-        t.v[s][j] = *reinterpret_cast<const typename A::Granule*>(at.k + a.g.S * D + j * 1024 + lane * A::GB);
-      }
+      for (int j = 0; j < A::NJ; ++j) t.k[s][j] = load_granule<PAST, typename A::Granule>(at.k + j * 1024 + lane * A::GB);
       t.ke[s] = *reinterpret_cast<const uint8_t*>(at.ke + (lane & 15));
+    }
+  };
+  auto load_v = [&](Tile& t, int tile) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const auto at = subs.at(2 * tile + s);
+#pragma unroll
+      for (int j = 0; j < A::NJ; ++j)
+        t.v[s][j] = load_granule<PAST, typename A::Granule>(at.k + a.g.S * D + j * 1024 + lane * A::GB);
       t.ve[s] = *reinterpret_cast<const uint32_t*>(at.ke + a.g.S + 4 * grp);
     }
   };
   uint32_t nan_seen = 0;
-  auto compute = [&](Tile& t, int tile) {
+  auto compute = [&](Tile& t, int tile, int next) {
     const int key0 = tile * 32;
     const bool edge = key0 + 31 > all_see;
+    const float ks[2] = {__uint_as_float(t.ke[0] << 23), __uint_as_float(t.ke[1] << 23)};
+    typename A::Scores s, x;
+    typename A::Weights p;
+    c.scores([&](int h, int i) { return k_operand(t.k[h][i / A::NE][2 * (i % A::NE)], t.k[h][i / A::NE][2 * (i % A::NE) + 1], ks[h]); }, s);
+    if constexpr (!kTwo) {
+      subs.look_up(next);
+      load_k(t, next);
+    }
     if (edge) {
       // what lies behind the last key is anything
 #pragma unroll
@@ -525,10 +547,6 @@ __global__ __launch_bounds__(256, D == 128 || MT == 2 ? 2 : 3) void q8_attn_kern
     for (int s = 0; s < 2; ++s)
 #pragma unroll
       for (int r = 0; r < 4; ++r) { ef[s][r] = exp_of(t.ve[s], r); iv[s][r] = inverse_of(t.ve[s], r); }
-    const float ks[2] = {__uint_as_float(t.ke[0] << 23), __uint_as_float(t.ke[1] << 23)};
-    typename A::Scores s, x;
-    typename A::Weights p;
-    c.scores([&](int h, int i) { return k_operand(t.k[h][i / A::NE][2 * (i % A::NE)], t.k[h][i / A::NE][2 * (i % A::NE) + 1], ks[h]); }, s);
     c.weigh(s, ef, a.scale, x);
     if (edge) c.hide(key0, lim, grp, x);
     if (c.over(x)) c.move_references(s, ef, key0, edge, lim, a.scale, grp, x);
@@ -537,35 +555,46 @@ __global__ __launch_bounds__(256, D == 128 || MT == 2 ? 2 : 3) void q8_attn_kern
       const u32x2 lo = v_values(t.v[0][i / A::W][i % A::W]), hi = v_values(t.v[1][i / A::W][i % A::W]);
       return __builtin_bit_cast(f16x8, (u32x4{lo[0], lo[1], hi[0], hi[1]}));
     }, p);
+    if constexpr (!kTwo) load_v(t, next);
   };
-  const int tile_end = (wk.key_last + 31) / 32;
-  int tile = wk.key_first / 32 + wave;
-  if (tile < tile_end) {
-    Tile t0, t1;
-    load(t0, tile);
-    for (;;) {
-      const int next = tile + 4;
-      load(t1, next < tile_end ? next : tile);
-      compute(t0, tile);
-      if (next >= tile_end) break;
-      tile = next + 4;
-      load(t0, tile < tile_end ? tile : next);
-      compute(t1, next);
-      if (tile >= tile_end) break;
+  const int tile_end = (wk.key_last + 31) / 32, tile_first = wk.key_first / 32 + wave;
+  Tile t0;
+  if (tile_first < tile_end) {
+    subs.look_up(tile_first);
+    load_k(t0, tile_first);
+    load_v(t0, tile_first);
+    if constexpr (kTwo) {
+      Tile t1;
+      for (int tile = tile_first;;) {
+        const int next = tile + 4;
+        subs.look_up(next < tile_end ? next : tile);
+        load_k(t1, next < tile_end ? next : tile);
+        load_v(t1, next < tile_end ? next : tile);
+        compute(t0, tile, next);
+        if (next >= tile_end) break;
+        tile = next + 4;
+        subs.look_up(tile < tile_end ? tile : next);
+        load_k(t0, tile < tile_end ? tile : next);
+        load_v(t0, tile < tile_end ? tile : next);
+        compute(t1, next, tile);
+        if (tile >= tile_end) break;
+      }
+    } else {
+      for (int tile = tile_first; tile < tile_end; tile += 4) compute(t0, tile, tile + 4 < tile_end ? tile + 4 : tile);
     }
   }
   if (__any(nan_seen != 0)) {
-    for (int again = wk.key_first / 32 + wave; again < tile_end; again += 4)
+    for (int again = tile_first; again < tile_end; again += 4)
       if (again * 32 + 31 > all_see) {
-        Tile t;
-        load(t, again);
+        subs.look_up(again);
+        load_v(t0, again);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
           for (int j = 0; j < A::NJ; ++j)
 #pragma unroll
-            for (int w = 0; w < A::W; ++w) t.v[s][j][w] &= first_bytes(wk.key_last - (again * 32 + 16 * s + 4 * grp));
-        c.add_nan(t.v, again * 32, lim, grp);
+            for (int w = 0; w < A::W; ++w) t0.v[s][j][w] &= first_bytes(wk.key_last - (again * 32 + 16 * s + 4 * grp));
+        c.add_nan(t0.v, again * 32, lim, grp);
       }
   }
 
@@ -869,7 +898,7 @@ __global__ __launch_bounds__(256) void q8_join_kernel(Q8AttnArgs a) {
 
 constexpr int kWideRows = 128, kFewRows = 64;
 
-Q8AttnPlan plan_q8_attention(const Q8Geom& g, int32_t num_q_heads, const BatchDev& b) {
+Q8AttnPlan plan_q8_attention(const Q8Geom& g, int32_t num_q_heads, const BatchDev& b, int32_t layers) {
   Q8AttnPlan p{};
   const int64_t G = num_q_heads / g.H, rows = G * b.max_new;
   p.too_large = rows >= (1ll << 30) || b.max_total_len > kMostKeys;
@@ -943,6 +972,7 @@ Q8AttnPlan plan_q8_attention(const Q8Geom& g, int32_t num_q_heads, const BatchDe
         l.slots = (held >> shift) + b.batch;
       }
     }
+    p.past_caches = l.q_tiles == 1 && kv_past_caches(g.D, keys / g.S * g.page_bytes, layers, keys / b.batch);
     finish(l, l.slots * l.q_tiles);
   }
   return p;
@@ -987,16 +1017,18 @@ static hipError_t launch(Q8AttnArgs a, const Q8AttnPlan& p, void* workspace, hip
   const dim3 grid = take(p.few);
   if (p.few.rows == 16) {
     if (a.chunk_shift < 31) {
-      q8_attn_kernel<D, 1, T, Numbered::kKeys><<<grid, block, 0, stream>>>(a);
+      if (p.past_caches) q8_attn_kernel<D, 1, T, Numbered::kKeys, true><<<grid, block, 0, stream>>>(a);
+      else q8_attn_kernel<D, 1, T, Numbered::kKeys, false><<<grid, block, 0, stream>>>(a);
       launch_join<D, T, 16, Numbered::kKeys>(a, stream);
     } else {
-      q8_attn_kernel<D, 1, T, Numbered::kUsers><<<grid, block, 0, stream>>>(a);
+      q8_attn_kernel<D, 1, T, Numbered::kUsers, false><<<grid, block, 0, stream>>>(a);
     }
   } else if (a.chunk_shift < 31) {
-    q8_attn_kernel<D, 2, T, Numbered::kKeys><<<grid, block, 0, stream>>>(a);
+    if (p.past_caches) q8_attn_kernel<D, 2, T, Numbered::kKeys, true><<<grid, block, 0, stream>>>(a);
+    else q8_attn_kernel<D, 2, T, Numbered::kKeys, false><<<grid, block, 0, stream>>>(a);
     launch_join<D, T, 32, Numbered::kKeys>(a, stream);
   } else {
-    q8_attn_kernel<D, 2, T, Numbered::kUsers><<<grid, block, 0, stream>>>(a);
+    q8_attn_kernel<D, 2, T, Numbered::kUsers, false><<<grid, block, 0, stream>>>(a);
   }
   return hipGetLastError();
 }
