@@ -154,7 +154,7 @@ struct Q8AttnLaunch {
   int32_t rows;              // query rows (tokens x query heads of a key head) of a tile
   int32_t above, upto;       // takes the users with more query rows than that, and at most so many
   int32_t q_tiles;           // few rows: tiles of the longest user's rows; many: stretches of the longest user's keys
-  int32_t tiles_each;        // many rows, users of one length: tiles of a user's; 0: by the table
+  bool    by_rank;           // many rows: the users' last tiles first
   int32_t chunk_shift;       // keys are cut into stretches of 2^chunk_shift tokens; 31: not cut
   int32_t part_rows;         // rows a stretch's partial result has room for
   int64_t slots;             // few rows: users, or stretches of all users; many: tiles of all users

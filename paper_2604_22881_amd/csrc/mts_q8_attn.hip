@@ -57,7 +57,7 @@ struct Q8AttnArgs {
   // of the launch, as in Q8AttnLaunch
   int32_t     above, upto;
   int32_t     q_tiles;
-  int32_t     tiles_each;
+  bool        by_rank;
   int32_t     chunk_shift;
   int32_t     part_rows;
   int64_t     slots;
@@ -353,7 +353,7 @@ __device__ __forceinline__ uint32_t first_bytes(int n) { return n >= 4 ? ~0u : n
 //   kUsers:  user, tile of rows                             few rows, keys not cut
 //   kKeys:   stretch of keys of all users, tile of rows     few rows: stretches of user u start at its first page's tokens / 2^shift + u
 //   kRows:   tile of rows of all users                      many rows: tiles of user u start at its first row / M + u, the last first
-//                                                           (users of one length: at tiles_each * u)
+//                                                           (by_rank: the last tiles of all users, then those before them, ..)
 //   kBoth:   stretch of a user's keys, tile of all users    many rows of few users, keys cut
 // so that both the stretches and the tiles of users of unlike size follow one another with one place per user left over at most,
 // and a place's user is found from a table that never falls.
@@ -367,8 +367,20 @@ struct Work {
   bool     partial;                // one of several stretches
 };
 template <int M>
-__device__ __forceinline__ int64_t first_tile(const Q8AttnArgs& a, int u) {
-  return a.tiles_each > 0 ? (int64_t)u * a.tiles_each : (int64_t)a.b.new_indptr[u] * a.G / M + u;
+__device__ __forceinline__ int64_t first_tile(const Q8AttnArgs& a, int u) { return (int64_t)a.b.new_indptr[u] * a.G / M + u; }
+// the place of the tile that `back` others of the user come behind, and the other way round
+template <int M>
+__device__ __forceinline__ int64_t tile_place(const Q8AttnArgs& a, int u, int64_t back) {
+  return a.by_rank ? back * a.b.batch + u : first_tile<M>(a, u) + back;
+}
+template <int M>
+__device__ __forceinline__ int64_t tile_at(const Q8AttnArgs& a, int64_t place, int& u) {
+  if (a.by_rank) {
+    u = (int)(place % a.b.batch);
+    return place / a.b.batch;
+  }
+  u = find_user(a.b.batch, place, [&](int s) -> int64_t { return first_tile<M>(a, s); });
+  return place - first_tile<M>(a, u);
 }
 __device__ __forceinline__ int64_t first_stretch(const Q8AttnArgs& a, int u) {
   return (((int64_t)a.b.page_indptr[u] * a.g.S) >> a.chunk_shift) + u;
@@ -384,8 +396,7 @@ __device__ __forceinline__ bool find_work(const Q8AttnArgs& a, Work& w) {
   if constexpr (kAllTiles) {
     const int64_t tile = N == Numbered::kBoth ? place % (uint32_t)a.slots : place;
     if constexpr (N == Numbered::kBoth) chunk = place / (uint32_t)a.slots;
-    u = a.tiles_each > 0 ? (int)(tile / a.tiles_each) : find_user(a.b.batch, tile, [&](int s) -> int64_t { return first_tile<M>(a, s); });
-    qt = tile - first_tile<M>(a, u);
+    qt = tile_at<M>(a, tile, u);
   } else {
     qt = place % (uint32_t)a.q_tiles;
     const int64_t slot = place / (uint32_t)a.q_tiles;
@@ -843,7 +854,7 @@ __global__ __launch_bounds__(256) void q8_join_kernel(Q8AttnArgs a) {
     place = slot * a.q_tiles + qt;
     next = a.q_tiles;
   } else {
-    place = first_tile<M>(a, u) + (rows + M - 1) / M - 1 - qt;
+    place = tile_place<M>(a, u, (rows + M - 1) / M - 1 - qt);
     next = a.slots;
     if (place < 0 || place >= a.slots || chunks > a.q_tiles) return;
   }
@@ -928,11 +939,14 @@ Q8AttnPlan plan_q8_attention(const Q8Geom& g, int32_t num_q_heads, const BatchDe
     l.upto = INT32_MAX;
     l.chunk_shift = 31;
     l.q_tiles = 1;
-    if (b.total_new == (int64_t)b.batch * b.max_new) {
-      l.tiles_each = (int)((rows + kWideRows - 1) / kWideRows);
-      l.slots = (int64_t)b.batch * l.tiles_each;
-    } else {
-      l.slots = (int64_t)b.total_new * G / kWideRows + b.batch;
+    l.slots = (int64_t)b.total_new * G / kWideRows + b.batch;
+    // Users of about one length: the long tiles of all of them start first, and what ends last is short.  us, tiles user after
+    // user / so: 8 first visits of 4096 x 8 (2 query heads each) of 128 719 / 674, 10 of 1943 x 2 (1) 101 / 74, 8 of 1432 x 16 (1)
+    // of 64 90 / 70, 8 of 241-1928 x 3 (3) in fp32 107 / 107.
+    const int64_t ranked = (int64_t)b.batch * ((rows + kWideRows - 1) / kWideRows);
+    if (ranked <= 2 * l.slots) {
+      l.by_rank = true;
+      l.slots = ranked;
     }
     const int64_t tiles = l.slots * g.H, seen = (held - b.total_new / 2) / b.batch;   // keys of a tile, about
     const bool few_tiles = tiles < 384 && b.max_total_len > 1024;
@@ -995,7 +1009,7 @@ static hipError_t launch(Q8AttnArgs a, const Q8AttnPlan& p, void* workspace, hip
     a.above = l.above;
     a.upto = l.upto;
     a.q_tiles = l.q_tiles;
-    a.tiles_each = l.tiles_each;
+    a.by_rank = l.by_rank;
     a.chunk_shift = l.chunk_shift;
     a.part_rows = l.part_rows;
     a.slots = l.slots;
