@@ -148,8 +148,9 @@ __global__ __launch_bounds__(256) void q8_move_kernel(Q8MoveArgs a) {
   const int h = wave % a.g.H;
   const int n_runs = MODE == MODE_APPEND ? a.b.batch : a.s.num_segs;
   auto first = [&](int s) -> int64_t { return MODE == MODE_APPEND ? (int64_t)a.b.new_indptr[s] : a.s.seg_tok_indptr[s]; };
-  auto base = [&](int s) -> int64_t { return (first(s) >> 4) + 2ll * s; };   // slots of the runs before s, or a few more
-  const int64_t slots = (first(n_runs) >> 4) + 2ll * n_runs;
+  const int64_t none = first(0);                             // rows ahead of the first run
+  auto base = [&](int s) -> int64_t { return ((first(s) - none) >> 4) + 2ll * s; };   // slots of the runs before s, or a few more
+  const int64_t slots = base(n_runs);
   const int64_t es_stride = (int64_t)a.g.H * D * es, head_row = (int64_t)h * D * es + (lane % LPR) * 16;
   for (int64_t slot = wave / a.g.H; slot < slots; slot += a.slots_in_flight) {
     const int s = find_user(n_runs, slot, base);
@@ -159,7 +160,7 @@ __global__ __launch_bounds__(256) void q8_move_kernel(Q8MoveArgs a) {
     if (n <= 0 || row0 < 0 || u < 0 || u >= a.b.batch) continue;
     const int64_t p0 = MODE == MODE_APPEND ? a.b.prefix_lens[u] : a.s.seg_pos[s];
     const int64_t sub = (p0 >> 4) + slot - base(s);
-    if (p0 < 0 || 16 * sub >= p0 + n) continue;
+    if (p0 < 0 || slot < base(s) || 16 * sub >= p0 + n) continue;
     const int64_t page0 = a.b.page_indptr[u], at = page0 + (sub >> a.g.sub_shift);
     if (page0 < 0 || at >= a.b.page_indptr[u + 1] || at >= a.b.total_pages) continue;
     const uint32_t page = (uint32_t)a.b.page_indices[at];

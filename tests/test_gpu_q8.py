@@ -193,6 +193,27 @@ def test_runs_are_stored_and_read_back(D, S, H, dtype):
     np.testing.assert_array_equal(s.pool(), s.image)
 
 
+def test_runs_behind_other_rows_of_the_buffer():
+    """Offsets that do not begin at 0: the runs of a part of a larger buffer."""
+    rng = np.random.default_rng(13)
+    H, D, S, skip = 2, 64, 16, 1003
+    s = Step(9, H, D, S, [70, 33], [0, 0], "bf16", fill=0x21)
+    runs = [(1, 0, 33), (0, 20, 50), (0, 0, 20)]
+    data = [rows(rng, (2, n, H, D), "bf16") for _, _, n in runs]
+    segs = SegmentList(*zip(*runs), DEV)
+    segs.seg_tok_indptr += skip
+    row = 2 * H * D
+    flat = torch.cat([torch.full((skip * row,), 3.0, dtype=torch.bfloat16, device=DEV), dev(np.concatenate([d.reshape(-1) for d in data]), "bf16")])
+    mts.mts_kv_unpack_q8(s.cache.desc, 0, B.MTS_BF16, flat, *segs.args(), s.batch.meta)
+    for (u, p, n), x in zip(runs, data):
+        R.store(s.image, s.w.user_pages(u), S, p, x)
+    np.testing.assert_array_equal(s.pool(), s.image)
+    out = torch.full((flat.numel(),), -7.0, dtype=torch.bfloat16, device=DEV)
+    mts.mts_kv_pack_q8(s.cache.desc, 0, B.MTS_BF16, out, *segs.args(), s.batch.meta)
+    assert (out[:skip * row] == -7.0).all()
+    np.testing.assert_array_equal(host(out[skip * row:]), np.concatenate([R.quantise(x)[2].reshape(-1) for x in data]))
+
+
 def test_many_users_and_runs():
     """More users than a wavefront has lanes, and more than the square of that."""
     rng = np.random.default_rng(11)
