@@ -35,6 +35,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -671,19 +672,192 @@ __global__ __launch_bounds__(256, (MT == 2 || (D == 128 && std::is_same<T, float
   }
 }
 
-// Many rows: the wavefronts have 16 MT rows each and go through the keys together.  A tile of 32 keys is converted to operands
+// Many rows, a wavefront's 32 and its sums, in 32x32x16 products: one query a lane, of each tile the 16 keys 8 b + 4 (lane / 32) + r
+// (b, r = 0 .. 3), the lane's accumulators in that order.
+template <int D, typename T>
+struct Wide {
+  static constexpr int KS = D / 16, DT = D / 32;
+  static constexpr bool kF32 = std::is_same<T, float>::value;
+  static constexpr int QP = kF32 ? 3 : 1, PP = kF32 ? 2 : 1;
+
+  bf16x8 q[KS][QP];
+  f32x16 o[DT];
+  float  neg_y, neg_r, l, E;       // as Attn's
+  bool   first, huge;
+
+  __device__ __forceinline__ void start() {
+    neg_y = neg_r = l = 0.f;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
+    E = kNoExp;
+    first = true;
+    huge = false;
+  }
+  __device__ __forceinline__ void load_queries(const char* row, int hf) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int d = 16 * s + 8 * hf;
+      if constexpr (kF32) {
+        const f32x4 a = *reinterpret_cast<const f32x4*>(row + d * 4), b = *reinterpret_cast<const f32x4*>(row + d * 4 + 16);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float x = j < 4 ? a[j & 3] : b[j & 3];
+          const __bf16 h = (__bf16)x;
+          const float r = x - (float)h;
+          const __bf16 m = (__bf16)r;
+          q[s][0][j] = h;
+          q[s][1 % QP][j] = m;
+          q[s][2 % QP][j] = (__bf16)(r - (float)m);
+        }
+      } else {
+        q[s][0] = *reinterpret_cast<const bf16x8*>(row + d * 2);
+      }
+    }
+  }
+  static __device__ __forceinline__ float both_halves_max(float v) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  }
+  __device__ __forceinline__ float total() const {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    return (__uint_as_float(a[0]) + __uint_as_float(a[1])) * exp2_of(E - 127.f);
+  }
+  static __device__ __forceinline__ int key_of(int r, int hf) { return 8 * (r >> 2) + 4 * hf + (r & 3); }
+
+  // k, v: the tile's operands; ef, iv: e + 127 and 2^-e of its keys of V; `edge`: some row does not see all keys; lim: the last
+  // key that this lane's query sees.
+  __device__ __forceinline__ void tile(const u32x4 (&k)[KS][64], const u32x4 (&v)[DT][2][64], const float* ef, const float* iv, int key0,
+                                       bool edge, int lim, float scale, int lane) {
+    const int hf = lane >> 5;
+    f32x16 s;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      const bf16x8 kk = __builtin_bit_cast(bf16x8, k[i][lane]);
+#pragma unroll
+      for (int p = QP - 1; p >= 0; --p) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, q[i][p], s, 0, 0, 0);
+    }
+    float x[16];
+    f32x4 e[4];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) e[b] = *reinterpret_cast<const f32x4*>(ef + 8 * b + 4 * hf);
+    auto weigh = [&] {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = __builtin_fmaf(s[r], scale, neg_r) + e[r >> 2][r & 3];
+    };
+    auto hide = [&] {
+      if (edge) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[r] = key0 + key_of(r, hf) > lim ? -__builtin_inff() : x[r];
+      }
+    };
+    weigh();
+    hide();
+    float most = x[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) most = fmaxf(most, x[r]);
+    if (first || huge || __any(most > kMost)) {
+      float e_most = E, y = -__builtin_inff();
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        e_most = fmaxf(e_most, e[r >> 2][r & 3]);
+        y = fmaxf(y, edge && key0 + key_of(r, hf) > lim ? -__builtin_inff() : rounded_product(s[r], scale));
+      }
+      e_most = both_halves_max(e_most);
+      y = both_halves_max(y);
+      const float e_step = exp2_of(E - e_most);
+      E = e_most;
+      // a query that sees none of the tile keeps its reference (0 at first: its sums are 0)
+      const float was = neg_y;
+      const bool seen = y > -__builtin_inff();
+      neg_y = seen ? (first ? kRef - y : fminf(was, kRef - y)) : was;
+      neg_r = neg_y - E;
+      const float f = first ? 0.f : exp2_of(neg_y - was) * e_step;
+      l *= f;
+#pragma unroll
+      for (int c = 0; c < DT; ++c) o[c] *= f;
+      huge = __any(__builtin_fabsf(neg_y) > kFused);
+      first = false;
+      if (huge) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[r] = (rounded_product(s[r], scale) + neg_y) + (e[r >> 2][r & 3] - E);
+      } else {
+        weigh();
+      }
+      hide();
+    }
+    f16x8 p[2][PP];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const f32x4 inv = *reinterpret_cast<const f32x4*>(iv + 8 * b + 4 * hf);
+      float w[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        w[r] = exp2_of(x[4 * b + r]);
+        l = __builtin_fmaf(w[r], inv[r], l);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; r += 2) {
+        const f16x2 a = __builtin_convertvector((f32x2{w[r], w[r + 1]}), f16x2);
+        p[b >> 1][0][4 * (b & 1) + r] = a[0];
+        p[b >> 1][0][4 * (b & 1) + r + 1] = a[1];
+        if constexpr (PP == 2) {
+          const f16x2 c = __builtin_convertvector((f32x2{w[r] - (float)a[0], w[r + 1] - (float)a[1]}), f16x2);
+          p[b >> 1][PP - 1][4 * (b & 1) + r] = c[0];
+          p[b >> 1][PP - 1][4 * (b & 1) + r + 1] = c[1];
+        }
+      }
+    }
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+      for (int c = 0; c < DT; ++c) {
+        const f16x8 vv = __builtin_bit_cast(f16x8, v[c][sub][lane]);
+#pragma unroll
+        for (int i = PP - 1; i >= 0; --i) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vv, p[sub][i], o[c], 0, 0, 0);
+      }
+  }
+
+  // As Attn's; v: the codes of V of a 16-token sub-block, of which the first n are keys.
+  __device__ __forceinline__ void add_nan(const char* v, int n, int key0, int lim, int lane) {
+#pragma unroll 1
+    for (int key = 0; key < n; ++key) {
+      uint32_t byte[DT], any = 0;
+#pragma unroll
+      for (int c = 0; c < DT; ++c) {
+        byte[c] = lane < 32 ? *reinterpret_cast<const uint8_t*>(v + q8_v_sub_index(key, 32 * c + lane, D)) & 0x7fu : 0u;
+        any |= byte[c] == 0x7fu;
+      }
+      if (!__any(any)) continue;
+#pragma unroll
+      for (int c = 0; c < DT; ++c) {
+        const u32x4 a{byte[c] == 0x7fu ? 0x7e00u : 0u, 0u, 0u, 0u}, one{0x3c00u, 0u, 0u, 0u};
+        const f32x16 nan = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, one), o[c], 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[c][r] = key0 + key <= lim ? nan[r] : o[c][r];
+      }
+    }
+  }
+};
+
+// Many rows: the wavefronts have 32 rows each and go through the keys together.  A tile of 32 keys is converted to operands
 // once, a quarter by each wavefront, into one of two stages in LDS, while the other is multiplied from.  Workgroups go to the 8
 // XCDs in turn, so that with the heads counted first the tiles of a (user, head) meet its keys in one XCD's L2 (8 heads), or two's.
-template <int D, int MT, typename T, Numbered N>
+template <int D, typename T, Numbered N>
 __global__ __launch_bounds__(256, 2) void q8_attn_wide_kernel(Q8AttnArgs a) {
-  using A = Attn<D, MT, T>;
-  constexpr int M = 64 * MT;
+  using A = Wide<D, T>;
+  constexpr int M = 128;
+  constexpr int GB = D >= 64 ? 16 : 8, NJ = D >= 64 ? D / 64 : 1, NE = GB / 8, W = GB / 4;   // as Attn's
+  using Granule = typename std::conditional<GB == 16, u32x4, u32x2>::type;
   struct Stage {
-    u32x4 k[2][A::KS][64];         // operands, one per lane
-    u32x4 v[A::DT][64];
-    float ef[2][16], iv[2][16];
+    u32x4 k[A::KS][64];            // operands, one per lane
+    u32x4 v[A::DT][2][64];
+    float ef[32], iv[32];
   };
-  __shared__ Stage stage[2];
+  __shared__ Stage stage[2][2];      // of two tiles each
   __shared__ int nan_seen[2];
   const int lane = threadIdx.x & 63, grp = lane >> 4, wave = uniform_int(threadIdx.x >> 6);
   Work wk;
@@ -691,136 +865,127 @@ __global__ __launch_bounds__(256, 2) void q8_attn_wide_kernel(Q8AttnArgs a) {
 
   A c;
   c.start();
-  const int first_row = wk.row_first + 16 * MT * wave, last_row = min(first_row + 16 * MT - 1, wk.row_last);
+  const int first_row = wk.row_first + 32 * wave, last_row = min(first_row + 31, wk.row_last);
   const int all_rows_see = wk.us.prefix + wk.row_first / a.G;
   const int all_see = wk.us.prefix + first_row / a.G, some_see = first_row <= wk.row_last ? wk.us.prefix + last_row / a.G : -1;
-  int lim[MT];
-#pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    const int row = min(first_row + 16 * m + (lane & 15), wk.row_last);
-    lim[m] = wk.us.prefix + row / a.G;
-    c.load_queries(m, a.q + row_at(a, wk, row) * D * (int64_t)sizeof(T), grp);
-  }
+  const int my_row = first_row + (lane & 31), known_row = min(my_row, wk.row_last);
+  const int lim = wk.us.prefix + known_row / a.G;
+  c.load_queries(a.q + row_at(a, wk, known_row) * D * (int64_t)sizeof(T), lane >> 5);
 
-  // this wavefront's part of a tile: K (0, 1) or V (2, 3) of one of the two sub-blocks
-  const int my_sub = wave & 1;
+  // this wavefront's part of a pair of tiles: K (0, 1) or V (2, 3) of one of the two
+  const int my_tile = wave & 1;
   const bool is_v = wave >= 2;
   SubBlocks<D> subs(a, wk);
   struct Raw {
-    typename A::Granule g[A::NJ];
-    uint32_t e;
+    Granule  g[2][NJ];
+    uint32_t e[2];
   };
-  const int codes_at = (is_v ? a.g.S * D : 0) + lane * A::GB, exps_at = (is_v ? a.g.S : 0) + (lane & 15);
-  auto load = [&](Raw& r, int tile) {
+  const int codes_at = (is_v ? a.g.S * D : 0) + lane * GB, exps_at = (is_v ? a.g.S : 0) + (lane & 15);
+  auto load = [&](Raw& r, int pair) {
+    const int tile = 2 * pair + my_tile;
     subs.look_up(tile);
-    const auto at = subs.at(2 * tile + my_sub);
 #pragma unroll
-    for (int j = 0; j < A::NJ; ++j) r.g[j] = *reinterpret_cast<const typename A::Granule*>(at.k + j * 1024 + codes_at);
-    r.e = *reinterpret_cast<const uint8_t*>(at.ke + exps_at);
-  };
-  const int tile_end = (wk.key_last + 31) / 32, tile_first = wk.key_first / 32;
-  auto convert = [&](Raw& r, int tile) {
-    const int key0 = tile * 32 + 16 * my_sub;
-    Stage& st = stage[(tile - tile_first) & 1];
-    if (is_v) {
-      uint32_t e = r.e;
-      if (tile * 32 + 31 > all_rows_see) {
-        if (key0 + (lane & 15) >= wk.key_last) e = (uint32_t)kNoExp;
-        const uint32_t keep = first_bytes(wk.key_last - (key0 + 4 * grp));
-        uint32_t any = 0;
+    for (int s = 0; s < 2; ++s) {
+      const auto at = subs.at(2 * tile + s);
 #pragma unroll
-        for (int j = 0; j < A::NJ; ++j)
-#pragma unroll
-          for (int w = 0; w < A::W; ++w) {
-            const uint32_t v = r.g[j][w] & keep, nan = nan_codes(v);
-            r.g[j][w] = v & ~nan;
-            any |= nan;
-          }
-        if (any) nan_seen[my_sub] = 1;
-      }
-#pragma unroll
-      for (int j = 0; j < A::NJ; ++j)
-#pragma unroll
-        for (int w = 0; w < A::W; ++w) reinterpret_cast<u32x2*>(&st.v[j * A::W + w][lane])[my_sub] = v_values(r.g[j][w]);
-      if (lane < 16) {
-        st.ef[my_sub][lane] = (float)e;
-        st.iv[my_sub][lane] = inverse_of(e, 0);
-      }
-    } else {
-      const float scale = __uint_as_float(r.e << 23);
-#pragma unroll
-      for (int i = 0; i < A::KS; ++i)
-        st.k[my_sub][i][lane] =
-            __builtin_bit_cast(u32x4, k_operand(r.g[i / A::NE][2 * (i % A::NE)], r.g[i / A::NE][2 * (i % A::NE) + 1], scale));
+      for (int j = 0; j < NJ; ++j) r.g[s][j] = *reinterpret_cast<const Granule*>(at.k + j * 1024 + codes_at);
+      r.e[s] = *reinterpret_cast<const uint8_t*>(at.ke + exps_at);
     }
   };
-  auto four_of = [&](const float (&from)[2][16], float (&to)[2][4]) {
+  const int pair_end = (wk.key_last + 63) / 64, pair_first = wk.key_first / 64;
+  auto convert = [&](Raw& r, int pair) {
+    const int tile = 2 * pair + my_tile;
+    Stage& st = stage[(pair - pair_first) & 1][my_tile];
+    if (is_v) {
+      if (tile * 32 + 31 > all_rows_see) {
+        uint32_t any = 0;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const f32x4 e = *reinterpret_cast<const f32x4*>(&from[h][4 * grp]);
+        for (int s = 0; s < 2; ++s) {
+          const int key0 = tile * 32 + 16 * s;
+          if (key0 + (lane & 15) >= wk.key_last) r.e[s] = (uint32_t)kNoExp;
+          const uint32_t keep = first_bytes(wk.key_last - (key0 + 4 * grp));
 #pragma unroll
-      for (int r = 0; r < 4; ++r) to[h][r] = e[r];
+          for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+              const uint32_t v = r.g[s][j][w] & keep, nan = nan_codes(v);
+              r.g[s][j][w] = v & ~nan;
+              any |= nan;
+            }
+        }
+        if (any) nan_seen[my_tile] = 1;
+      }
+      // a lane has four keys, group grp of the sub-block, of dim lane % 16 of each 16: of 32 dims' operand half of lane
+      // 32 (grp % 2) + the dim
+      const int to = 32 * (grp & 1) + (lane & 15);
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int w = 0; w < W; ++w)
+            reinterpret_cast<u32x2*>(&st.v[j * (W / 2) + w / 2][s][to + 16 * (w & 1)])[grp >> 1] = v_values(r.g[s][j][w]);
+        if (lane < 16) {
+          st.ef[16 * s + lane] = (float)r.e[s];
+          st.iv[16 * s + lane] = inverse_of(r.e[s], 0);
+        }
+      }
+    } else {
+      // and of K one token's 8 dims twice, or once
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const float scale = __uint_as_float(r.e[s] << 23);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int e = 0; e < NE; ++e) {
+            const int eight = (4 * j + grp) * NE + e;        // of the row's eights of dims
+            st.k[eight >> 1][32 * (eight & 1) + 16 * s + (lane & 15)] =
+                __builtin_bit_cast(u32x4, k_operand(r.g[s][j][2 * e], r.g[s][j][2 * e + 1], scale));
+          }
+      }
     }
   };
   if (threadIdx.x < 2) nan_seen[threadIdx.x] = 0;
   __syncthreads();
   Raw raw;
-  load(raw, tile_first);
-  convert(raw, tile_first);
-  load(raw, tile_first + 1);
+  load(raw, pair_first);
+  convert(raw, pair_first);
+  load(raw, pair_first + 1);
   __syncthreads();
-  for (int tile = tile_first; tile < tile_end; ++tile) {
-    const Stage& st = stage[(tile - tile_first) & 1];
-    if (tile + 1 < tile_end) {
-      convert(raw, tile + 1);
-      load(raw, tile + 2);
+  for (int pair = pair_first; pair < pair_end; ++pair) {
+    if (pair + 1 < pair_end) {
+      convert(raw, pair + 1);
+      load(raw, pair + 2);
     }
-    const int key0 = tile * 32;
-    if (key0 <= some_see) {
-      const bool edge = key0 + 31 > all_see;
-      typename A::Scores s, x;
-      typename A::Weights p;
-      float ef[2][4], iv[2][4];
-      four_of(st.ef, ef);
-      four_of(st.iv, iv);
-      c.scores([&](int h, int i) { return __builtin_bit_cast(bf16x8, st.k[h][i][lane]); }, s);
-      c.weigh(s, ef, a.scale, x);
-      if (edge) c.hide(key0, lim, grp, x);
-      if (c.over(x)) c.move_references(s, ef, key0, edge, lim, a.scale, grp, x);
-      c.weights(x, iv, p);
-      c.add_products([&](int i) { return __builtin_bit_cast(f16x8, st.v[i][lane]); }, p);
+#pragma unroll 1
+    for (int i = 0; i < 2; ++i) {
+      const Stage& st = stage[(pair - pair_first) & 1][i];
+      const int key0 = 64 * pair + 32 * i;
+      if (key0 <= some_see && key0 < wk.key_last) c.tile(st.k, st.v, st.ef, st.iv, key0, key0 + 31 > all_see, lim, a.scale, lane);
     }
     __syncthreads();
   }
+  const int tile_end = (wk.key_last + 31) / 32, tile_first = wk.key_first / 32;
   if (uniform_int(nan_seen[0] | nan_seen[1]) != 0) {
     for (int again = tile_first; again < tile_end; ++again)
       if (again * 32 + 31 > all_rows_see) {
-        typename A::Granule v[2][A::NJ];
         subs.look_up(again);
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const auto at = subs.at(2 * again + s);
-          const uint32_t keep = first_bytes(wk.key_last - (again * 32 + 16 * s + 4 * grp));
-#pragma unroll
-          for (int j = 0; j < A::NJ; ++j) {
-            v[s][j] = *reinterpret_cast<const typename A::Granule*>(at.k + a.g.S * D + j * 1024 + lane * A::GB);
-#pragma unroll
-            for (int w = 0; w < A::W; ++w) v[s][j][w] &= keep;
-          }
-        }
-        c.add_nan(v, again * 32, lim, grp);
+#pragma unroll 1
+        for (int s = 0; s < 2; ++s)
+          c.add_nan(subs.at(2 * again + s).k + a.g.S * D, min(wk.key_last - (again * 32 + 16 * s), 16), again * 32 + 16 * s, lim, lane);
       }
   }
+  const float l = c.total(), e = exp2_of(c.E - 127.f);
+  if (my_row > wk.row_last) return;
 #pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    const float l = c.total(m), e = exp2_of(c.E - 127.f);
-    const int row = first_row + 16 * m + (lane & 15);
-    if (row > wk.row_last) continue;
+  for (int i = 0; i < A::DT; ++i)
 #pragma unroll
-    for (int i = 0; i < A::DT; ++i) store_sums<D, T>(a, wk, row, 16 * i + 4 * grp, c.o[m][i] * e, 1.f / l);
-    if (wk.partial && grp == 0)
-      *reinterpret_cast<f32x2*>(a.part_ml + (wk.item * a.part_rows + (row - wk.row_first)) * 2) = f32x2{l == 0.f ? -__builtin_inff() : kRef - c.neg_y[m], l};
-  }
+    for (int b = 0; b < 4; ++b)
+      store_sums<D, T>(a, wk, my_row, 32 * i + A::key_of(4 * b, lane >> 5),
+                       f32x4{c.o[i][4 * b], c.o[i][4 * b + 1], c.o[i][4 * b + 2], c.o[i][4 * b + 3]} * e, 1.f / l);
+  if (wk.partial && lane < 32)
+    *reinterpret_cast<f32x2*>(a.part_ml + (wk.item * a.part_rows + (my_row - wk.row_first)) * 2) = f32x2{l == 0.f ? -__builtin_inff() : kRef - c.neg_y, l};
 }
 
 // Joins the stretches of a row's keys, in an order that only their number decides: one wavefront or four per (token, query head),
@@ -1021,10 +1186,10 @@ static hipError_t launch(Q8AttnArgs a, const Q8AttnPlan& p, void* workspace, hip
   if (p.wide.on) {
     const dim3 grid = take(p.wide);
     if (a.chunk_shift < 31) {
-      q8_attn_wide_kernel<D, 2, T, Numbered::kBoth><<<grid, block, 0, stream>>>(a);
+      q8_attn_wide_kernel<D, T, Numbered::kBoth><<<grid, block, 0, stream>>>(a);
       launch_join<D, T, kWideRows, Numbered::kBoth>(a, stream);
     } else {
-      q8_attn_wide_kernel<D, 2, T, Numbered::kRows><<<grid, block, 0, stream>>>(a);
+      q8_attn_wide_kernel<D, T, Numbered::kRows><<<grid, block, 0, stream>>>(a);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !p.few.on) return e;
