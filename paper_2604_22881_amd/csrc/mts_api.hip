@@ -762,7 +762,7 @@ static int32_t check_q_heads(const mts::Q8Geom& g, int32_t num_q_heads) {
 }
 
 static int32_t too_large_q8(const mts::BatchDev& b) {
-  return fail(MTS_ERR_UNSUPPORTED, "batch %d x max_new %d query rows make more tiles than one call holds (2^31), or max_total_len %d "
+  return fail(MTS_ERR_UNSUPPORTED, "batch %d x max_new %d query rows make more tiles than one call holds (2^24), or max_total_len %d "
               "exceeds 2^30", b.batch, b.max_new, b.max_total_len);
 }
 
@@ -838,8 +838,8 @@ int32_t mts_qk_norm_rope(const mts_qk_desc* d, const void* q, const void* k, voi
   if (!q || !k || !q_out || !k_out) return fail(MTS_ERR_INVALID_ARG, "q / k / q_out / k_out is NULL");
   if (!aligned(q, 16) || !aligned(k, 16) || !aligned(q_out, 16) || !aligned(k_out, 16))
     return fail(MTS_ERR_INVALID_ARG, "q / k / q_out / k_out is not 16-byte aligned");
-  if (((int64_t)d->num_q_heads + d->num_k_heads) * b.total_new >= (1ll << 32))
-    return fail(MTS_ERR_UNSUPPORTED, "%d tokens of %d + %d heads are more rows than one call takes (2^32)", b.total_new, d->num_q_heads, d->num_k_heads);
+  if (((int64_t)d->num_q_heads + d->num_k_heads) * b.total_new >= (1ll << 32) || b.total_new >= (1 << 26))
+    return fail(MTS_ERR_UNSUPPORTED, "%d tokens of %d + %d heads are more than one call takes (2^26 tokens, 2^32 rows)", b.total_new, d->num_q_heads, d->num_k_heads);
   a.q = (const char*)q; a.k = (const char*)k; a.q_out = (char*)q_out; a.k_out = (char*)k_out;
   a.q_weight = (const char*)d->q_weight; a.k_weight = (const char*)d->k_weight; a.freqs = d->freqs; a.eps = d->eps;
   a.Hq = d->num_q_heads; a.Hk = d->num_k_heads; a.D = d->head_dim; a.rot_dim = d->rot_dim;

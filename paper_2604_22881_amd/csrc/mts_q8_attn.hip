@@ -10,9 +10,10 @@
 // two is a bf16 value, so the logits are those of the stored values with fp32 sums; rows of K meet that power
 // in the conversion.  S^T leaves a lane with 8 tokens of one query, the ones whose codes of V it holds.
 //
-// V's power of two varies along the index that P V sums over, so it goes to the weight: with Y a reference of the logits
-// (base 2) and E of V's exponents e, both of them per query and wavefront,
+// V's power of two e varies along the index that P V sums over, so it goes to the weight: with references Y of the logits
+// (base 2) and E, both of them per query and wavefront,
 //   w_j = 2^(y_j - Y + e_j - E),  O = sum w_j code_j,  l = sum w_j 2^(E - e_j),  out = 2^E O / l.
+// Y is some largest y_j and E some largest y_j - Y + e_j, so that a large row of V which nothing weighs takes no bits from the others.
 // w is rounded to fp16 for the product (11 bits, half a step 2^-12: next to it the output's own rounding to bf16, 2^-9, is
 // what counts) and taken into l unrounded; weights are scaled so that the references' own is 2^10 and nothing above 2^-24 of it
 // is below fp16's normal numbers.  Y and E move only when some w would exceed 2^15, and all sums are then
@@ -143,8 +144,8 @@ struct Attn {
   f32x4  o[MT][DT];
   float  neg_y[MT];                // -(Y - kRef)
   float  neg_r[MT];                // the same less E, for a fused subtraction
-  float  l[MT];                    // sums of this lane's keys, times 2^(-127 - E) ..
-  float  E;                        // reference of V's exponents, + 127
+  float  E[MT];                    // + 127
+  float  l[MT];                    // sums of this lane's keys, times 2^(127 - E)
   bool   first;                    // no keys yet
   bool   huge;                     // some reference is beyond what an fma may be exact to
 
@@ -152,10 +153,10 @@ struct Attn {
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
       neg_y[m] = neg_r[m] = l[m] = 0.f;
+      E[m] = kNoExp;
 #pragma unroll
       for (int i = 0; i < DT; ++i) o[m][i] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    E = kNoExp;
     first = true;
     huge = false;
   }
@@ -235,31 +236,32 @@ struct Attn {
   // References that hold for this tile too, and the sums scaled to them.
   __device__ __forceinline__ void move_references(const Scores& s, const float (&ef)[2][4], int key0, bool edge, const int (&lim)[MT],
                                                   float scale, int grp, Scores& x) {
-    float e_most = E;
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) e_most = fmaxf(e_most, ef[h][r]);
-    e_most = over_groups(e_most, [](float a, float b) { return fmaxf(a, b); });
-    const float e_step = exp2_of(E - e_most);
-    E = e_most;
     float largest = 0.f;
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-      float y = -__builtin_inff();
+      float y = -__builtin_inff(), py[2][4];
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          y = fmaxf(y, edge && key0 + 16 * h + 4 * grp + r > lim[m] ? -__builtin_inff() : rounded_product(s[h][m][r], scale));
+        for (int r = 0; r < 4; ++r) {
+          py[h][r] = edge && key0 + 16 * h + 4 * grp + r > lim[m] ? -__builtin_inff() : rounded_product(s[h][m][r], scale);
+          y = fmaxf(y, py[h][r]);
+        }
       y = over_groups(y, [](float a, float b) { return fmaxf(a, b); });
-      // a query that sees none of the tile keeps its reference (0 at first: its sums are 0)
-      const float was = neg_y[m];
+      // a query that sees none of the tile keeps its references (0 and the least at first: its sums are 0)
+      const float was = neg_y[m], e_was = E[m];
       const bool seen = y > -__builtin_inff();
       const float now = seen ? (first ? kRef - y : fminf(was, kRef - y)) : was;
-      const float f = first ? 0.f : exp2_of(now - was) * e_step;
+      float e = kNoExp;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) e = fmaxf(e, (py[h][r] + now) + (ef[h][r] - kRef));
+      e = over_groups(e, [](float a, float b) { return fmaxf(a, b); });
+      E[m] = first ? e : fmaxf(e, e_was + (now - was));
+      const float f = first ? 0.f : exp2_of((now - was) + (e_was - E[m]));
       neg_y[m] = now;
-      neg_r[m] = now - E;
+      neg_r[m] = now - E[m];
       l[m] *= f;
 #pragma unroll
       for (int c = 0; c < DT; ++c) o[m][c] *= f;
@@ -273,7 +275,7 @@ struct Attn {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) x[h][m][r] = (rounded_product(s[h][m][r], scale) + neg_y[m]) + (ef[h][r] - E);
+          for (int r = 0; r < 4; ++r) x[h][m][r] = (rounded_product(s[h][m][r], scale) + neg_y[m]) + (ef[h][r] - E[m]);
     } else {
       weigh(s, ef, scale, x);
     }
@@ -342,7 +344,7 @@ struct Attn {
 
   // sum of the weights over all keys, in units of the output's
   __device__ __forceinline__ float total(int m) const {
-    return over_groups(l[m], [](float a, float b) { return a + b; }) * exp2_of(E - 127.f);
+    return over_groups(l[m], [](float a, float b) { return a + b; }) * exp2_of(E[m] - 127.f);
   }
 };
 
@@ -613,16 +615,16 @@ __global__ __launch_bounds__(256, (MT == 2 || (D == 128 && std::is_same<T, float
   // The four wavefronts' sums: each takes a quarter of the dims (of 32 dims two take half) from the others.
   constexpr int DT = A::DT, OWNERS = DT < 4 ? DT : 4, OWN = DT / OWNERS;
   __shared__ f32x4 xo[OWNERS * 3 * OWN * MT * 64];
-  __shared__ float xy[4][M], xl[4][M], xe[4];
+  __shared__ float xy[4][M], xl[4][M], xe[4][M];
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     const float l = c.total(m);
     if (grp == 0) {
-      xy[wave][16 * m + lane] = l == 0.f ? -__builtin_inff() : kRef - c.neg_y[m];   // none of its keys seen
+      xy[wave][16 * m + lane] = l == 0.f ? -__builtin_inff() : -c.neg_y[m];   // none of its keys seen
       xl[wave][16 * m + lane] = l;
+      xe[wave][16 * m + lane] = c.E[m] - 127.f;
     }
   }
-  if (lane == 0) xe[wave] = c.E - 127.f;
 #pragma unroll
   for (int w = 0; w < OWNERS; ++w)
     if (w != wave) {
@@ -644,9 +646,9 @@ __global__ __launch_bounds__(256, (MT == 2 || (D == 128 && std::is_same<T, float
     float f[4], l = 0.f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      f[w] = exp2_of(xy[w][in_tile] - ref);
-      l = __builtin_fmaf(xl[w][in_tile], f[w], l);
-      f[w] *= exp2_of(xe[w]);
+      const float below = xy[w][in_tile] - ref;
+      l = __builtin_fmaf(xl[w][in_tile], exp2_of(below), l);
+      f[w] = exp2_of(below + xe[w][in_tile]);
     }
     const float inv = 1.f / l;
 #pragma unroll
@@ -682,7 +684,7 @@ struct Wide {
 
   bf16x8 q[KS][QP];
   f32x16 o[DT];
-  float  neg_y, neg_r, l, E;       // as Attn's
+  float  neg_y, neg_r, E, l;       // as Attn's
   bool   first, huge;
 
   __device__ __forceinline__ void start() {
@@ -760,22 +762,23 @@ struct Wide {
 #pragma unroll
     for (int r = 1; r < 16; ++r) most = fmaxf(most, x[r]);
     if (first || huge || __any(most > kMost)) {
-      float e_most = E, y = -__builtin_inff();
+      float y = -__builtin_inff();
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        e_most = fmaxf(e_most, e[r >> 2][r & 3]);
-        y = fmaxf(y, edge && key0 + key_of(r, hf) > lim ? -__builtin_inff() : rounded_product(s[r], scale));
+        x[r] = edge && key0 + key_of(r, hf) > lim ? -__builtin_inff() : rounded_product(s[r], scale);
+        y = fmaxf(y, x[r]);
       }
-      e_most = both_halves_max(e_most);
       y = both_halves_max(y);
-      const float e_step = exp2_of(E - e_most);
-      E = e_most;
-      // a query that sees none of the tile keeps its reference (0 at first: its sums are 0)
-      const float was = neg_y;
+      const float was = neg_y, e_was = E;
       const bool seen = y > -__builtin_inff();
       neg_y = seen ? (first ? kRef - y : fminf(was, kRef - y)) : was;
+      float e_most = kNoExp;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) e_most = fmaxf(e_most, (x[r] + neg_y) + (e[r >> 2][r & 3] - kRef));
+      e_most = both_halves_max(e_most);
+      E = first ? e_most : fmaxf(e_most, e_was + (neg_y - was));
       neg_r = neg_y - E;
-      const float f = first ? 0.f : exp2_of(neg_y - was) * e_step;
+      const float f = first ? 0.f : exp2_of((neg_y - was) + (e_was - E));
       l *= f;
 #pragma unroll
       for (int c = 0; c < DT; ++c) o[c] *= f;
@@ -985,7 +988,7 @@ __global__ __launch_bounds__(256, 2) void q8_attn_wide_kernel(Q8AttnArgs a) {
       store_sums<D, T>(a, wk, my_row, 32 * i + A::key_of(4 * b, lane >> 5),
                        f32x4{c.o[i][4 * b], c.o[i][4 * b + 1], c.o[i][4 * b + 2], c.o[i][4 * b + 3]} * e, 1.f / l);
   if (wk.partial && lane < 32)
-    *reinterpret_cast<f32x2*>(a.part_ml + (wk.item * a.part_rows + (my_row - wk.row_first)) * 2) = f32x2{l == 0.f ? -__builtin_inff() : kRef - c.neg_y, l};
+    *reinterpret_cast<f32x2*>(a.part_ml + (wk.item * a.part_rows + (my_row - wk.row_first)) * 2) = f32x2{l == 0.f ? -__builtin_inff() : -c.neg_y, l};
 }
 
 // Joins the stretches of a row's keys, in an order that only their number decides: one wavefront or four per (token, query head),
@@ -1084,7 +1087,7 @@ Q8AttnPlan plan_q8_attention(const Q8Geom& g, int32_t num_q_heads, const BatchDe
   auto finish = [&](Q8AttnLaunch& l, int64_t places) {
     l.on = true;
     l.items = places * g.H;
-    p.too_large |= l.items >= (1ll << 31);
+    p.too_large |= l.items >= (1ll << 24);             // a launch's threads are counted in 32 bits
     if (l.chunk_shift < 31) {
       const int64_t bytes = (l.items * l.part_rows * (g.D + 2) * (int64_t)sizeof(float) + 255) / 256 * 256;
       if (bytes > p.ws_bytes) p.ws_bytes = bytes;

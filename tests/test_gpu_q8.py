@@ -525,3 +525,167 @@ def test_decode_steps_of_a_serving_loop():
     out = torch.empty(segs.total_tokens * 2 * H * D, dtype=torch.float32, device=DEV)
     mts.mts_kv_pack_q8(cache.desc, 0, B.MTS_F32, out, *segs.args(), batch.meta)
     np.testing.assert_array_equal(host(out), np.concatenate([g.reshape(-1) for g in grown]))
+
+
+# ---- many rows: the keys shared by a workgroup's wavefronts -----------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,prefix,new", [(64, [300, 0, 64], [1, 1, 1]), (128, [3000], [2]), (32, [300, 20], [140, 3]), (128, [40], [150]),
+                                          (64, [1500], [130])])
+def test_large_rows_of_v_without_weight_leave_the_others_theirs(D, prefix, new, dtype):
+    """Rows of V at 2^50 whose logits lie 400 below the others': the outputs are those of the other keys, each with all bits."""
+    rng = np.random.default_rng(40)
+    H, G, S = 2, 1, 16
+    s = Step(40, H, D, S, prefix, new, dtype)
+    s.fill_prefixes(rng, 0.5)
+    q = rows(rng, (s.w.total_new, H * G, D), dtype, 0.0) * 0.25
+    q[..., 0] = 1.0
+
+    def with_large(n):
+        x = rows(rng, (2, n, H, D), dtype, 0.5)
+        x[0, ..., 0] = 0.0
+        far = rng.random((n, H)) < 0.3
+        x[0][far] = 0.0
+        x[0, ..., 0][far] = -400.0
+        x[1][far] *= 2.0 ** 50
+        return x
+    runs = [(u, 0, p) for u, p in enumerate(prefix) if p > 0]
+    data = [with_large(n) for _, _, n in runs]
+    s.unpack(runs, data)
+    for (u, p, n), x in zip(runs, data):
+        R.store(s.image, s.w.user_pages(u), S, p, x)
+    x = with_large(s.w.total_new)
+    for u in range(len(new)):                                # every query has a key of its own size
+        if prefix[u] == 0:
+            x[:, s.w.new_indptr[u]] = 0.5
+    s.append(dev(x[0], dtype), dev(x[1], dtype))
+    s.expect_append(x[0], x[1])
+    got = s.attention(dev(q, dtype), G, 1.0)
+    assert s.check_attention(got, q, G, 1.0) <= 1.0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 130])
+def test_weights_that_are_subnormal_in_fp16_count(n, dtype):
+    """4000 keys at 2^-27 of the largest weight, which alone make up half of the dims: 2^-17 where the largest is 2^10."""
+    H, D, T = 1, 64, 4000
+    s = Step(41, H, D, 16, [T], [n], dtype, fill=0)
+    k, v = np.zeros((T + n, H, D)), np.ones((T + n, H, D))
+    k[:T, 0, 0] = -27.0 * np.log(2.0)
+    v[T:, :, :32] = 0.0
+    k = W.bf16_bits_to_f32(W.f32_to_bf16_bits(k.astype(np.float32))).astype(np.float64)
+    s.unpack([(0, 0, T)], [np.stack([k[:T], v[:T]]).astype(np.float32)])
+    s.append(dev(k[T:], dtype), dev(v[T:], dtype))
+    R.store(s.image, s.w.user_pages(0), 16, 0, np.stack([k, v]))
+    q = np.zeros((n, H, D), np.float32)
+    q[:, 0, 0] = 1.0
+    got = s.attention(dev(q, dtype), 1, 1.0)
+    kv = R.load(s.image, s.w.user_pages(0), 16, T + n, H, D)
+    out, mag, lsum = R.attention(q, kv, T, 1.0)
+    # a weight is off by 2^-35 of the largest product of a weight and its row's 2^e at most (all rows of V have one e here): over all
+    # keys 4130 * 2^-35 of p <= 1, times the values' 1
+    bound = R.attention_bound(out, mag, lsum, T + n, D, dtype == "f32") + (T + n) * 2.0 ** -35
+    assert out[0, 0, 0] > 1e-5
+    assert (np.abs(got - out) <= bound).all()
+    assert (np.abs(got - out)[..., :32] <= 2.0 ** -7 * out[..., :32]).all()    # 2^-25 of 2^-17, and a rounding
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_of_very_different_size_under_many_rows(dtype):
+    attend(42, 2, 4, 64, 16, [700, 90], [40, 70], dtype, spread=6.0)
+    attend(43, 1, 1, 128, 32, [1500], [140], dtype, spread=6.0)
+
+
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_huge_logits_under_many_rows(D):
+    rng = np.random.default_rng(44)
+    H, S, T, n = 2, 16, 200, 130
+    s = Step(44, H, D, S, [T], [n], "f32")
+    kv = rows(rng, (2, T, H, D), "f32", 0.0)
+    kv[1] *= 2.0 ** rng.integers(-6, 7, (T, H, 1))
+    kv[0] *= 0.25
+    kv[0, 77], kv[0, 150, 1] = 1.0, 1.0
+    k_new, v_new = np.zeros((n, H, D), np.float32), rows(rng, (n, H, D), "f32")
+    s.unpack([(0, 0, T)], [kv])
+    s.append(dev(k_new, "f32"), dev(v_new, "f32"))
+    v = R.quantise(kv[1])[2]
+    for big in (1e9, 1e20, 1e30):
+        got = s.attention(dev(np.full((n, H, D), big, np.float32), "f32"), 1, 1.0)
+        np.testing.assert_array_equal(got[:, 0], np.broadcast_to(v[77, 0], (n, D)))       # the weight is a power of two
+        np.testing.assert_allclose(got[:, 1], np.broadcast_to((v[77, 1] + v[150, 1]) / 2, (n, D)), rtol=0,
+                                   atol=(2.0 ** -22 + 6 * 2.0 ** -24) * np.abs(v[[77, 150], 1]).max())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,prefix,new", [(32, [50, 20, 0], [140, 9, 150]), (128, [50, 20, 0], [140, 9, 150]), (64, [1100, 1000], [140, 130])])
+def test_nan_and_infinity_under_many_rows(D, prefix, new, dtype):
+    """Uncut and in stretches: NaN among a user's own new keys reaches the queries from it on, and no other."""
+    rng = np.random.default_rng(45)
+    H, G, S = 2, 2, 16
+    s = Step(45, H, D, S, prefix, new, dtype)
+    s.fill_prefixes(rng)
+    n, at = s.w.total_new, s.w.new_indptr
+    k, v = rows(rng, (n, H, D), dtype), rows(rng, (n, H, D), dtype)
+    k[at[0] + 100, 0, 5] = np.nan
+    v[at[0] + 11, 1, 3] = np.inf
+    v[at[0] + 63, 1, D - 1] = np.nan
+    v[at[0] + 64, 1, 0] = np.nan
+    v[at[-1] - 1, 0, 0] = np.nan                             # the last token of the last user
+    v[at[-2] + 4, 1, D - 1] = -np.inf
+    k[at[-2] + 127, 1, 0] = np.nan
+    s.append(dev(k, dtype), dev(v, dtype))
+    s.expect_append(k, v)
+    q = rows(rng, (n, H * G, D), dtype, 0.3)
+    got = s.attention(dev(q, dtype), G)
+    for u in range(len(new)):
+        kv = R.load(s.image, s.w.user_pages(u), S, int(s.w.total_lens[u]), H, D)
+        ref, mag, lsum = R.attention(q[at[u]:at[u + 1]], kv, prefix[u], D ** -0.5)
+        part = got[at[u]:at[u + 1]]
+        np.testing.assert_array_equal(np.isnan(part), np.isnan(ref))
+        fine = np.isfinite(ref)
+        assert (np.abs(part - ref)[fine] <= R.attention_bound(ref, mag, lsum, kv.shape[1], D, dtype == "f32")[fine]).all()
+
+
+def test_what_lies_behind_the_last_key_under_many_rows():
+    for prefix, new in (([5, 37, 0], [130, 3, 200]), ([1100], [131])):
+        got = [attend(46, 2, 2, 64, 32, prefix, new, "bf16", fill=fill, users=[0])[2] for fill in (0xFF, 0x00, 0x7F, 0x01)]
+        for g in got[1:]:
+            np.testing.assert_array_equal(g, got[0])
+
+
+def test_bad_page_ids_and_short_page_lists_under_many_rows():
+    rng = np.random.default_rng(47)
+    s = Step(47, 2, 64, 16, [400, 1200], [130, 140], "bf16", fill=0)
+    s.fill_prefixes(rng)
+    k = dev(rows(rng, (270, 2, 64), "bf16"), "bf16")
+    s.append(k, k)
+    s.batch.page_indices[3] = 1 << 30
+    s.batch.page_indices[4] = -1
+    s.batch.prefix_lens[1] = 500000                          # more than its pages hold
+    q = dev(rows(rng, (270, 4, 64), "bf16"), "bf16")
+    assert np.isfinite(s.attention(q, 2)[:130]).all()
+
+
+@pytest.mark.parametrize("prefix,new", [([900, 0], [140, 200]), ([3000, 1200, 40], [140, 1, 200])])
+def test_many_rows_repeat_on_another_stream_and_from_a_graph(prefix, new):
+    """Uncut; and cut, with users of few rows in a launch of their own."""
+    s, q, got = attend(48, 2, 4, 64, 16, prefix, new, "bf16", users=[0])
+    t = dev(q, "bf16")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(s.attention(t, 4, stream=side), got)
+    n = mts.mts_attn_q8_workspace_bytes(s.cache.desc, 8, s.batch.meta)
+    ws = torch.empty(max(n, 256), dtype=torch.uint8, device=DEV)
+    out = torch.empty_like(t)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mts.mts_attn_incremental_q8(s.cache.desc, 0, B.MTS_BF16, 8, t, out, s.batch.meta, 0.0, ws, n)
+    rng = np.random.default_rng(49)
+    for i in range(4):
+        t.copy_(dev(rows(rng, q.shape, "bf16", 0.3), "bf16"))
+        eager = s.attention(t, 4)
+        ws.fill_(77)
+        out.fill_(77)
+        graph.replay()
+        torch.cuda.synchronize()
+        np.testing.assert_array_equal(host(out), eager)
