@@ -374,9 +374,9 @@ int32_t mts_kv_pack_q8(const mts_cache_desc* cache, int32_t layer, int32_t row_d
  * behind a long history (the keys are cut into stretches that are joined by a second kernel) to a whole
  * history at once.  The result is that of the stored values: logits from exact products with fp32 sums,
  * fp32 softmax statistics and accumulators.  bf16 rows: weights take part in the weighted sum of V rounded to
- * fp16 (half a step: 2^-12 of the weight); fp32 rows: queries with 24 bits, weights with 22.  A weight times its row's
- * 2^e below 2^-34 of the largest such product so far may count as 0 in the weighted sum.  Keys behind a query do not reach
- * its output, whatever they hold.
+ * fp16 (half a step: 2^-12 of the weight); fp32 rows: queries (up to 2^127) with 24 bits, weights with 22.  Either may be off by
+ * 2^-33 of the largest product of a weight and its row's 2^e that a query has, over that e.  Rows of V of one head more than
+ * 2^90 apart in size are outside this.  Keys behind a query do not reach its output, whatever they hold.
  * The workspace is as for mts_attn_incremental; a call given less than mts_attn_q8_workspace_bytes is
  * refused with MTS_ERR_WORKSPACE.  max_total_len <= 2^30; mts_attn_set_tuning has no bearing on this call.
  */

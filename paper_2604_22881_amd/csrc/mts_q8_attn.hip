@@ -15,9 +15,8 @@
 //   w_j = 2^(y_j - Y + e_j - E),  O = sum w_j code_j,  l = sum w_j 2^(E - e_j),  out = 2^E O / l.
 // Y is some largest y_j and E some largest y_j - Y + e_j, so that a large row of V which nothing weighs takes no bits from the others.
 // w is rounded to fp16 for the product (11 bits, half a step 2^-12: next to it the output's own rounding to bf16, 2^-9, is
-// what counts) and taken into l unrounded; weights are scaled so that the references' own is 2^10 and nothing above 2^-24 of it
-// is below fp16's normal numbers.  Y and E move only when some w would exceed 2^15, and all sums are then
-// scaled.  y_j - Y is one fma; where logits are so large that their rounding is a matter of whole powers of two, the
+// what counts) and taken into l unrounded; weights are scaled so that the references' own is 2^8 and nothing above 2^-22 of it
+// is below fp16's normal numbers.  Y and E move only when some w would leave fp16, and all sums are then scaled.  y_j - Y is one fma; where logits are so large that their rounding is a matter of whole powers of two, the
 // product is rounded first, as the reference was, so that the largest logit's weight is the reference's.  fp32 rows: queries as three bf16 parts, weights as two
 // fp16 ones, which keep 24 and 22 bits.
 //
@@ -42,8 +41,12 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-constexpr float kRef = 10.f;       // log2 of the weight of the references
-constexpr float kMost = 15.f;      // of the largest weight (fp16 ends below 2^16)
+// log2 of the weight of the references, and of the largest, which fp16's 65504 bounds.  The room between them is for later keys
+// that weigh more, for which all sums would be scaled; below the references, fp16's half step of 2^-25 is 2^-33 of theirs.
+// us a call with 5, 7, 9 bits of room: 8 first visits of 4096 x 8 (2 query heads each) of 128 706, 682, 666; 120 users' 48 rows x 5
+// (8) of 64 in fp32 45.6, 44.9, 44.4.
+constexpr float kRef = 8.f;
+constexpr float kMost = 15.99f;
 // A reference is a rounded logit, an fma's product is not: up to this size the two differ by 1/4 at most.
 constexpr float kFused = 4194304.f;
 constexpr float kNoExp = (float)(kQ8ExpMin + 127);   // what keys without a row count as
