@@ -157,6 +157,7 @@ struct Q8AttnLaunch {
   bool    by_rank;           // many rows: the users' last tiles first
   int32_t chunk_shift;       // keys are cut into stretches of 2^chunk_shift tokens; 31: not cut
   int32_t part_rows;         // rows a stretch's partial result has room for
+  int32_t user_rows;         // few rows: most of a user
   int64_t slots;             // few rows: users, or stretches of all users; many: tiles of all users
   int64_t items;             // workgroups
 };

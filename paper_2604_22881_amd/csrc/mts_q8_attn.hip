@@ -65,6 +65,7 @@ struct Q8AttnArgs {
   bool        by_rank;
   int32_t     chunk_shift;
   int32_t     part_rows;
+  int32_t     user_rows;
   int64_t     slots;
   float*      part_o;              // [item][part_rows][D]
   float*      part_ml;             // [item][part_rows][2]
@@ -994,8 +995,9 @@ __global__ __launch_bounds__(256, 2) void q8_attn_wide_kernel(Q8AttnArgs a) {
     *reinterpret_cast<f32x2*>(a.part_ml + (wk.item * a.part_rows + (my_row - wk.row_first)) * 2) = f32x2{l == 0.f ? -__builtin_inff() : -c.neg_y, l};
 }
 
-// Joins the stretches of a row's keys, in an order that only their number decides: one wavefront or four per (token, query head),
-// D / 4 lanes to a stretch, so that 2 to 32 of them are read at once and a long history's hundreds take no chain of round trips.
+// Joins the stretches of a row's keys, in an order that only their number decides: one wavefront or four per (user, row, head) of
+// few rows (a number that needs no table) or (token, query head) of many, D / 4 lanes to a stretch, so that 2 to 32 of them are
+// read at once and a long history's hundreds take no chain of round trips.
 template <int D, typename T, int M, Numbered N, int WAVES>
 __global__ __launch_bounds__(256) void q8_join_kernel(Q8AttnArgs a) {
   constexpr int L = D / 4, P = 64 / L;                       // lanes of a stretch, stretches of a wavefront
@@ -1004,15 +1006,25 @@ __global__ __launch_bounds__(256) void q8_join_kernel(Q8AttnArgs a) {
   const int lane = threadIdx.x & 63, wave = uniform_int(threadIdx.x >> 6);
   const int Hq = a.g.H * a.G;
   const uint32_t unit = WAVES == 4 ? blockIdx.x : blockIdx.x * 4 + wave;
-  const int token = (int)(unit / (uint32_t)Hq), hq = (int)(unit % (uint32_t)Hq);
-  if (token >= a.b.total_new) return;
-  const int u = find_user(a.b.batch, token, [&](int s) -> int64_t { return a.b.new_indptr[s]; });
-  const UserSpan us = user_span(a.b, a.g.S, u);
-  const int i = token - us.row0;
-  if (i < 0 || i >= us.n) return;
-  const int h = hq / a.G;
-  const int64_t row = (int64_t)i * a.G + hq % a.G, rows = (int64_t)us.n * a.G;
-  if (rows <= a.above || rows > a.upto) return;
+  int u, h;
+  int64_t row;
+  UserSpan us;
+  if constexpr (N == Numbered::kKeys) {
+    h = (int)(unit % (uint32_t)a.g.H);
+    row = unit / (uint32_t)a.g.H % (uint32_t)a.user_rows;
+    u = (int)(unit / (uint32_t)a.g.H / (uint32_t)a.user_rows);
+    if (u >= a.b.batch) return;
+    us = user_span(a.b, a.g.S, u);
+  } else {
+    const int token = (int)(unit / (uint32_t)Hq), hq = (int)(unit % (uint32_t)Hq);
+    if (token >= a.b.total_new) return;
+    u = find_user(a.b.batch, token, [&](int s) -> int64_t { return a.b.new_indptr[s]; });
+    us = user_span(a.b, a.g.S, u);
+    h = hq / a.G;
+    row = (int64_t)(token - us.row0) * a.G + hq % a.G;
+  }
+  const int64_t rows = (int64_t)us.n * a.G;
+  if (row < 0 || row >= rows || rows <= a.above || rows > a.upto) return;
   const int64_t qt = row / M, last = (qt + 1) * M < rows ? (qt + 1) * M : rows;
   const int keys = keys_of(us, (int)last - 1, a.G);
   const int chunks = (int)(((int64_t)keys + (1ll << a.chunk_shift) - 1) >> a.chunk_shift);
@@ -1067,7 +1079,7 @@ __global__ __launch_bounds__(256) void q8_join_kernel(Q8AttnArgs a) {
   }
   if (lane >= L) return;
   const f32x4 v = acc * (1.f / l);
-  const int64_t dst = ((int64_t)token * Hq + hq) * D + 4 * lane;
+  const int64_t dst = ((us.row0 + row / a.G) * Hq + h * a.G + row % a.G) * D + 4 * lane;
   if constexpr (std::is_same<T, float>::value) {
     *reinterpret_cast<f32x4*>(a.out + dst * 4) = v;
   } else {
@@ -1142,6 +1154,7 @@ Q8AttnPlan plan_q8_attention(const Q8Geom& g, int32_t num_q_heads, const BatchDe
     l.upto = wide ? kFewRows : INT32_MAX;
     l.rows = most_rows > 16 ? 32 : 16;
     l.part_rows = (int)(most_rows < l.rows ? most_rows : l.rows);
+    l.user_rows = (int)most_rows;
     l.q_tiles = (int)((most_rows + l.rows - 1) / l.rows);
     l.chunk_shift = 31;
     l.slots = b.batch;
@@ -1169,8 +1182,8 @@ static void launch_join(const Q8AttnArgs& a, hipStream_t stream) {
   // By the stretches of the longest user: a chain of many loads is shared by four wavefronts, a chain of a few too where the
   // rows do not fill the chip.  us a call, one wavefront / four: 70 K keys x 4 heads, 274 stretches 28.7 / 12.6; 55 users' single
   // tokens, 11 stretches, 165 rows 12.6 / 12.0; 2 users' 3 K tokens, 13 stretches, 15 K rows 31 / 50.
-  const int64_t units = (int64_t)a.b.total_new * a.g.H * a.G;
-  if ((a.b.max_total_len >> a.chunk_shift) >= (units <= 512 ? 8 : 32)) q8_join_kernel<D, T, M, N, 4><<<dim3((unsigned)units), dim3(256), 0, stream>>>(a);
+  const int64_t rows = (int64_t)a.b.total_new * a.g.H * a.G, units = N == Numbered::kKeys ? (int64_t)a.b.batch * a.user_rows * a.g.H : rows;
+  if ((a.b.max_total_len >> a.chunk_shift) >= (rows <= 512 ? 8 : 32)) q8_join_kernel<D, T, M, N, 4><<<dim3((unsigned)units), dim3(256), 0, stream>>>(a);
   else q8_join_kernel<D, T, M, N, 1><<<dim3((unsigned)((units + 3) / 4)), dim3(256), 0, stream>>>(a);
 }
 
@@ -1184,6 +1197,7 @@ static hipError_t launch(Q8AttnArgs a, const Q8AttnPlan& p, void* workspace, hip
     a.by_rank = l.by_rank;
     a.chunk_shift = l.chunk_shift;
     a.part_rows = l.part_rows;
+    a.user_rows = l.user_rows;
     a.slots = l.slots;
     a.part_o = (float*)workspace;
     a.part_ml = (float*)workspace + l.items * l.part_rows * D;
