@@ -377,6 +377,8 @@ int32_t mts_kv_pack_q8(const mts_cache_desc* cache, int32_t layer, int32_t row_d
  * fp16 (half a step: 2^-12 of the weight); fp32 rows: queries (up to 2^127) with 24 bits, weights with 22.  Either may be off by
  * 2^-33 of the largest product of a weight and its row's 2^e that a query has, over that e.  Rows of V of one head more than
  * 2^90 apart in size are outside this.  Keys behind a query do not reach its output, whatever they hold.
+ * Here, in mts_kv_append_q8 and in mts_qk_norm_rope meta's four sizes may be bounds, as in a captured step that is padded: rows from
+ * new_indptr[B] on stay as they are.
  * The workspace is as for mts_attn_incremental; a call given less than mts_attn_q8_workspace_bytes is
  * refused with MTS_ERR_WORKSPACE.  max_total_len <= 2^30; mts_attn_set_tuning has no bearing on this call.
  */
@@ -394,7 +396,7 @@ int32_t mts_attn_incremental_q8(const mts_cache_desc* cache, int32_t layer, int3
  *   rotation  of rot_dim / 2 pairs by t_i = p * freqs[i]:  (a, b) -> (a cos t - b sin t, b cos t + a sin t)
  *             pair i is dims (i, i + rot_dim/2) (MTS_ROPE_HALVES) or (2i, 2i + 1) (MTS_ROPE_NEIGHBOURS);
  *             dims from rot_dim on are not rotated.  t_i is computed in 64 bits.
- * Computed in fp32 and rounded to the type once.  Reads meta's prefix_lens, new_indptr and scalars only.
+ * Computed in fp32 (also the sum of squares) and rounded to the type once.  Reads meta's prefix_lens, new_indptr and scalars only.
  * A token's heads are contiguous rows of head_dim; from one token to the next lie *_token_stride elements
  * (0: heads * head_dim; a multiple of 16 bytes, at least that).  An output may be its own input (same address,
  * same stride), but may not overlap the inputs otherwise.

@@ -71,7 +71,9 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkArgs a, BatchDev b,
   const int token = (int)(unit / parts), part = (int)(unit % parts);
   if (token >= b.total_new) return;
   const int u = find_user(b.batch, token, [&](int s) -> int64_t { return b.new_indptr[s]; });
-  const int64_t pos = (int64_t)b.prefix_lens[u] + (token - b.new_indptr[u]);
+  const int first = b.new_indptr[u];
+  if (token < first || token >= b.new_indptr[u + 1]) return;          // a padded step's rows behind the last user stay as they are
+  const int64_t pos = (int64_t)b.prefix_lens[u] + (token - first);
 
   // the lane's two groups of four dims, and its four pairs
   const int rot = a.rot_dim;

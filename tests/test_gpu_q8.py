@@ -689,3 +689,52 @@ def test_many_rows_repeat_on_another_stream_and_from_a_graph(prefix, new):
         graph.replay()
         torch.cuda.synchronize()
         np.testing.assert_array_equal(host(out), eager)
+
+
+@pytest.mark.parametrize("prefix,new,used", [([40, 9, 100], [3, 2, 4], [1, 0, 2]), ([2000, 100], [40, 60], [1, 37]),
+                                             ([300, 20, 0], [140, 150, 3], [130, 0, 1]), ([3000, 40], [200, 200], [129, 1])])
+def test_a_padded_step(prefix, new, used):
+    """Sizes that are bounds, as a captured step has them: the device's tables end earlier, and the rows behind them stay as they are.
+    Norm + rotation, append and attention against the same calls of the step's own size, bit for bit in the pool."""
+    rng = np.random.default_rng(50)
+    H, G, D, S = 2, 2, 64, 16
+    Hq, n_used, dtype = H * G, sum(used), "bf16"
+    freqs = torch.from_numpy(10000.0 ** (-np.arange(D // 2) / (D / 2))).to(DEV)
+    desc = mts.QkDesc(B.MTS_BF16, Hq, H, D, 0, 0, 0, 0, 0, 0, B.MTS_NORM_RMS, 1e-6, freqs.data_ptr(), D, B.MTS_ROPE_HALVES)
+    q, k, v = (rows(rng, (sum(new), h, D), dtype, 0.5) for h in (Hq, H, H))
+    hist = [rows(rng, (2, p, H, D), dtype) for p in prefix]
+    got = []
+    for lengths in (used, new):
+        s = Step(50, H, D, S, prefix, new, dtype, fill=0x22)
+        s.unpack([(u, 0, p) for u, p in enumerate(prefix) if p], [x for x in hist if x.size])
+        b = s.batch
+        if lengths is used:                                  # the step's own sizes, the same pages
+            b = DeviceBatch(s.w.page_indptr, s.w.page_indices, prefix, np.concatenate([[0], np.cumsum(used)]), DEV)
+        else:
+            b.new_indptr.copy_(torch.from_numpy(np.concatenate([[0], np.cumsum(used)]).astype(np.int32)))
+        n = sum(lengths)
+        qo, out = (torch.full((n, Hq, D), -7.0, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        ko = torch.full((n, H, D), -7.0, dtype=torch.bfloat16, device=DEV)
+        mts.mts_qk_norm_rope(desc, dev(q[:n], dtype), dev(k[:n], dtype), qo, ko, b.meta)
+        mts.mts_kv_append_q8(s.cache.desc, 0, B.MTS_BF16, ko, dev(v[:n], dtype), b.meta)
+        nb = mts.mts_attn_q8_workspace_bytes(s.cache.desc, Hq, b.meta)
+        ws = torch.empty(max(nb, 256), dtype=torch.uint8, device=DEV)
+        mts.mts_attn_incremental_q8(s.cache.desc, 0, B.MTS_BF16, Hq, qo, out, b.meta, 0.0, ws, nb)
+        torch.cuda.synchronize()
+        for t in (qo, ko, out):
+            assert (t[n_used:] == -7.0).all()
+        got.append([host(t[:n_used]) for t in (qo, ko, out)] + [s.pool()])
+    for a, b in zip(got[0][:2], got[1][:2]):
+        np.testing.assert_array_equal(a, b)
+    np.testing.assert_array_equal(got[0][3], got[1][3])
+    # the keys may be cut otherwise: each is within its bound of the same value
+    s = Step(50, H, D, S, prefix, used, dtype)
+    for u in range(len(used)):
+        a, b = sum(used[:u]), sum(used[:u + 1])
+        if b == a:
+            continue
+        kv = np.concatenate([R.quantise(hist[u])[2], R.quantise(np.stack([got[0][1][a:b], v[a:b].astype(np.float64)]))[2]], 1)
+        ref, mag, lsum = R.attention(got[0][0][a:b], kv, prefix[u], D ** -0.5)
+        bound = R.attention_bound(ref, mag, lsum, kv.shape[1], D, False)
+        for g in got:
+            assert (np.abs(g[2][a:b] - ref) <= bound).all()
