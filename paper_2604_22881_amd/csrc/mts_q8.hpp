@@ -3,10 +3,11 @@
 //
 // A row (one token, one head, K or V) of D values is kept as one exponent e and D e4m3 codes: value =
 // code * 2^e.  e is the smallest integer with amax <= 464 * 2^e over the row's finite values, held in
-// [-60, 60]: the smallest for which amax still rounds to a code (448 and the next step, 480, meet at 464).  Scaling by a power of two is exact in fp32, bf16 and fp16, so that codes do not depend on
-// how a kernel computes them, every stored value is a bf16 value, and a row that is read back and
-// stored again gives the same bytes: its largest value is 448 * 2^e or less, and more than 464 * 2^(e-1),
-// for which the smaller exponent would not do (above 232 the codes are 240 and up).
+// [-60, 60]: the smallest for which amax still rounds to a code (448 and the next step, 480, meet at
+// 464).  Scaling by a power of two is exact in fp32, bf16 and fp16, so that codes do not depend on how a
+// kernel computes them, every stored value is a bf16 value, and a row that is read back and stored again
+// gives the same bytes: its largest value is 448 * 2^e or less, and more than 464 * 2^(e-1), for which the
+// smaller exponent would not do (above 232 the codes are 240 and up).
 // The exponents' range is held where sums of 2^17 tokens' weights times 2^e, and their inverses, stay
 // finite in fp32; values above 448 * 2^60 saturate, below 2^-70 they are 0.
 //

@@ -1,14 +1,15 @@
 // Incremental attention over the 8-bit pool (mts_q8.hpp), query heads sharing key heads:
 //   out[i, h] = sum_j softmax_j(sm_scale * q[i, h] . K[j, h / G]) V[j, h / G],  j in [0, prefix + i].
 //
-// The query rows of a (user, key head) are its new tokens times the G query heads of the key head; a workgroup takes a tile
-// of 16 or 32 of them and a stretch of the user's keys, its four wavefronts every fourth tile of 32 keys, each with all the
-// rows.  Their sums are joined through LDS, and where the keys are cut into several stretches (a few rows behind a
-// long history would leave most of the chip idle) a second kernel joins the stretches.
+// The query rows of a (user, key head) are its new tokens times the G query heads of the key head.  Of few rows a workgroup takes a
+// tile of 16 or 32 and a stretch of the user's keys, its four wavefronts every fourth tile of 32 keys, each with all the rows;
+// their sums are joined through LDS.  Of many (128 and more) it takes 128, 32 a wavefront, and all go through the same keys.
+// Where the keys are cut into several stretches (a few rows behind a long history would leave most of the chip idle) a second
+// kernel joins them.
 //
-// Operand flow, 16x16x32 matrix instructions: S^T = K Q^T in bf16 and O^T = V^T P^T in fp16.  A code times its row's power of
-// two is a bf16 value, so the logits are those of the stored values with fp32 sums; rows of K meet that power
-// in the conversion.  S^T leaves a lane with 8 tokens of one query, the ones whose codes of V it holds.
+// Operand flow: S^T = K Q^T in bf16 and O^T = V^T P^T in fp16.  A code times its row's power of two is a bf16 value, so the
+// logits are those of the stored values with fp32 sums; rows of K meet that power in the conversion.  S^T leaves a lane with
+// tokens of one query, the ones whose codes of V it holds (16x16x32 instructions, few rows) or reads (32x32x16, many).
 //
 // V's power of two e varies along the index that P V sums over, so it goes to the weight: with references Y of the logits
 // (base 2) and E, both of them per query and wavefront,
@@ -22,7 +23,8 @@
 //
 // Bound: few rows, reading K and V once (2 (D + 1) bytes a token); many, the vector instructions beside the products (per weight
 // an fma, an addition, a maximum, an exponential, an fma and half a conversion, and per code of the tile half a conversion
-// that the 16 or 32 rows share).
+// that the tile's rows share).  Measured: 32 users' single tokens behind 6-16 K keys x 8 heads of 128, 722 MB, 130 us with its
+// join (5.6 TB/s); first visits of 4096 tokens x 8 users x 8 (2 query heads each) of 128, 550 GFLOP, 665 us (827 TFLOP/s).
 #include <type_traits>
 
 #include "mts_internal.hpp"
@@ -484,7 +486,8 @@ __device__ __forceinline__ void store_sums(const Q8AttnArgs& a, const Work& w, i
   }
 }
 
-// Few rows: every wavefront has all of them and every fourth tile of the keys.  PAST: K and V past the caches' retention, where a
+// Few rows: every wavefront has all of them and every fourth tile of the keys, so that the rows' operands stay in registers, K and V
+// go there from memory without a barrier, and a tile of one row costs what 16 do (the products are not what bounds it).  PAST: K and V past the caches' retention, where a
 // call reads nothing of them twice (kv_past_caches): 32 users x 10 K keys x 8 heads of 128 141 -> 130 us.
 template <int D, int MT, typename T, Numbered N, bool PAST>
 __global__ __launch_bounds__(256, (MT == 2 || (D == 128 && std::is_same<T, float>::value)) ? 2 : 3) void q8_attn_kernel(Q8AttnArgs a) {
@@ -850,8 +853,10 @@ struct Wide {
   }
 };
 
-// Many rows: the wavefronts have 32 rows each and go through the keys together.  A tile of 32 keys is converted to operands
-// once, a quarter by each wavefront, into one of two stages in LDS, while the other is multiplied from.  Workgroups go to the 8
+// Many rows: the wavefronts have 32 rows each and go through the keys together.  Two tiles of 32 keys are converted to operands
+// once, K or V of one by each wavefront, into one of two stages in LDS, while the other is multiplied from: codes are converted
+// once for 128 rows, and a barrier stands behind 64 keys (behind 32, in 16x16x32 instructions, first visits of 4096 x 8 took 730 us
+// where 680).  Of their time 46 % are vector instructions and 30 % products.  Workgroups go to the 8
 // XCDs in turn, so that with the heads counted first the tiles of a (user, head) meet its keys in one XCD's L2 (8 heads), or two's.
 template <int D, typename T, Numbered N>
 __global__ __launch_bounds__(256, 2) void q8_attn_wide_kernel(Q8AttnArgs a) {

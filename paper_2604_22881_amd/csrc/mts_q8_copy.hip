@@ -3,7 +3,8 @@
 //   unpack - contiguous runs (a restored history), quantised as they are written
 //   pack   - the inverse: stored rows read back as values into contiguous runs
 //
-// All three are bound by memory: es + 1 + 1/D bytes per element and a few instructions each.  A wavefront takes a 16-token
+// All three are bound by memory: es + 1 + 1/D bytes per element and a few instructions each (read back, 48 users' 819 MB 145 us,
+// 5.6 TB/s; stored and read back, 24 users' 1.47 GB 240 us, 6.1 TB/s).  A wavefront takes a 16-token
 // sub-block of one head, K and V.  On the rows' side its lanes take 16 bytes each, whole rows next to one another, on the pool's side
 // granules of K and four-token groups of V; codes change sides through 16 rows of the wavefront's own in LDS, 16 bytes longer
 // than D so that no access meets a bank twice.  V's [dim][4 tokens] order is a 4x4 transposition of bytes among four

@@ -1,7 +1,8 @@
 // Norm of a step's queries and keys, head by head, and their rotation by position, in one pass:
 //   y = x / sqrt(mean(x^2) + eps) * w;   (a, b) -> (a cos t - b sin t, b cos t + a sin t),  t = position * freq[pair].
 //
-// Bound by memory: each element is read and written once.  A row of D elements is D / 8 lanes, each with 8 of them such that
+// Bound by memory: each element is read and written once (39 K tokens x 24 heads of 128 in bf16, 470 MB, 93 us: 5.1 TB/s; one
+// token a user, 4 us).  A row of D elements is D / 8 lanes, each with 8 of them such that
 // both of a pair are in one lane: dims 4 j .. + 3 of the first and of the second half of the rotated dims, or 8 neighbours.
 // The dims behind the rotated ones are shared out in the same way.  A wavefront takes one token and goes through
 // heads, so that the angles are found once for several rows.

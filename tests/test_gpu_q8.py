@@ -738,3 +738,47 @@ def test_a_padded_step(prefix, new, used):
         bound = R.attention_bound(ref, mag, lsum, kv.shape[1], D, False)
         for g in got:
             assert (np.abs(g[2][a:b] - ref) <= bound).all()
+
+
+def test_pools_and_strides_beyond_32_bits():
+    """A layer of 5.3 GB and tokens 2 GB apart: the same bytes and results as in a small pool from rows that follow one another."""
+    rng = np.random.default_rng(51)
+    H, G, D, S, prefix, new = 8, 2, 128, 64, [300, 70, 1500], [1, 2, 1]
+    Hq, n, dtype = H * G, sum(new), "bf16"
+    small = Step(51, H, D, S, prefix, new, dtype, fill=0x33)
+    w = small.w
+    pages = 40000
+    cache = PagedKVCache(1, pages, S, H, D, "e4m3", DEV, fill_byte=0x33)
+    assert cache.page_bytes * pages > 1 << 32
+    ids = np.asarray(w.page_indices)
+    far = pages - 1 - ids                                    # the last pages of the pool, backwards
+    batch = DeviceBatch(w.page_indptr, far, prefix, w.new_indptr, DEV)
+    q, k, v = (rows(rng, (n, h, D), dtype, 0.5) for h in (Hq, H, H))
+    hist = [rows(rng, (2, p, H, D), dtype) for p in prefix]
+    runs = [(u, 0, p) for u, p in enumerate(prefix)]
+    stride = 1 << 30
+    apart = torch.empty((n - 1) * stride + (Hq + 2 * H) * D, dtype=torch.bfloat16, device=DEV)
+    qkv = apart.as_strided((n, Hq + 2 * H, D), (stride, D, 1))
+    qkv.copy_(dev(np.concatenate([q, k, v], 1), dtype))
+    freqs = torch.from_numpy(10000.0 ** (-np.arange(D // 2) / (D / 2))).to(DEV)
+    got = []
+    for c, b, s in ((small.cache, small.batch, 0), (cache, batch, stride)):
+        segs = SegmentList(*zip(*runs), DEV)
+        mts.mts_kv_unpack_q8(c.desc, 0, B.MTS_BF16, dev(np.concatenate([x.reshape(-1) for x in hist]), dtype), *segs.args(), b.meta)
+        qi, ki, vi = (qkv, qkv[:, Hq:], qkv[:, Hq + H:]) if s else (dev(q, dtype), dev(k, dtype), dev(v, dtype))
+        qo = torch.empty(n, Hq, D, dtype=torch.bfloat16, device=DEV)
+        ko = ki if s else torch.empty(n, H, D, dtype=torch.bfloat16, device=DEV)      # in place where they lie apart
+        desc = mts.QkDesc(B.MTS_BF16, Hq, H, D, s, s, 0, s, 0, 0, B.MTS_NORM_RMS, 1e-6, freqs.data_ptr(), D, B.MTS_ROPE_HALVES)
+        mts.mts_qk_norm_rope(desc, qi, ki, qo, ko, b.meta)
+        mts.mts_kv_append_q8(c.desc, 0, B.MTS_BF16, ko, vi, b.meta, s, s)
+        out = torch.empty_like(qo)
+        nb = mts.mts_attn_q8_workspace_bytes(c.desc, Hq, b.meta)
+        ws = torch.empty(max(nb, 256), dtype=torch.uint8, device=DEV)
+        mts.mts_attn_incremental_q8(c.desc, 0, B.MTS_BF16, Hq, qo, out, b.meta, 0.0, ws, nb)
+        back = torch.empty(segs.total_tokens * 2 * H * D, dtype=torch.bfloat16, device=DEV)
+        mts.mts_kv_pack_q8(c.desc, 0, B.MTS_BF16, back, *segs.args(), b.meta)
+        torch.cuda.synchronize()
+        image = c.layer_bytes(0)[torch.from_numpy(ids if c is small.cache else far).long().to(DEV)]
+        got.append([host(qo), host(out), host(back), image.cpu().numpy()])
+    for a, b in zip(*got):
+        np.testing.assert_array_equal(a, b)
