@@ -1163,14 +1163,27 @@ Q8AttnPlan plan_q8_attention(const Q8Geom& g, int32_t num_q_heads, const BatchDe
     l.q_tiles = (int)((most_rows + l.rows - 1) / l.rows);
     l.chunk_shift = 31;
     l.slots = b.batch;
-    // About 2048 workgroups, each with at least 256 keys.  us a call with 1024, 2048, 4096 workgroups: 32 users x 10 K keys x 8
-    // heads of 128 144, 140, 142; 32 rows each 166, 164, 172; 64 x 1.5 K x 8 of 64 28.8, 27.8, 31.4; with 128 keys and more 60 K keys
-    // x 4 15.3 where 12.4.  Short histories are not cut, which saves the second launch: 1 user's 900 keys x 8 heads 9.3 / 7.9, 40
-    // users' 700 x 8 of 128 19.6 / 14.1.
+    // Workgroups of at least 256 keys: about 2048, which even out users of unlike length; of little work (keys x heads x tiles)
+    // fewer, since each takes some us to begin and to end; of very much 4096.  Two tiles of 128 dims: one full round (two on each
+    // of 256 CUs) if some length of stretches gives it.  us a call with 2048 / by this rule: 10 users of 6-48 K keys x 2 heads of 64
+    // 20.4 / 17.2, 5 of 9-20 K x 3 27.6 / 21.1, 29 of 0.4-2.6 K x 8 of 128 26.3 / 27.0, 44 of 4-12 K x 1 of 32 15.6 / 14.6, 50 of
+    // 11-20 K x 8 82.7 / 77.5; 32 rows each behind 32 x 10 K x 8 of 128 159 / 146, 64 behind 111 x 3.7 K x 2 86.6 / 67.9.  With 1024
+    // for 64 x 1.5 K x 8 of 64 28.3 where 27.4, for 32 x 10 K x 8 of 128 141 where 130, with 4096 135.  Short histories are not cut,
+    // which saves the second launch: 1 user's 900 keys x 8 heads 9.3 / 7.9, 40 users' 700 x 8 of 128 19.6 / 14.1.
     const int64_t pairs = (int64_t)l.q_tiles * g.H;
     if (b.batch * pairs < 4096 && b.max_total_len > 1024) {
+      const int64_t work = keys * pairs;
+      int64_t most = 2048;
+      if (!wide && work < 1 << 19) most = 512;
+      else if (!wide && l.rows == 16) most = work < 3 << 18 ? 1024 : work < 1 << 22 ? 2048 : 4096;
       int shift = 8;
-      while (shift < 30 && (keys >> shift) * pairs > 2048) ++shift;
+      while (shift < 30 && (keys >> shift) * pairs > most) ++shift;
+      if (!wide && l.rows == 32 && g.D == 128) {
+        auto items = [&](int s) { return ((keys >> s) + b.batch / 2) * pairs; };   // half of a user's last stretch is empty
+        int s = shift;
+        while (s < 30 && items(s) > 512) ++s;
+        if (items(s) >= 384) shift = s;
+      }
       if ((1ll << shift) < b.max_total_len) {
         l.chunk_shift = shift;
         l.slots = (held >> shift) + b.batch;
