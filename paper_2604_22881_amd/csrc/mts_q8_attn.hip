@@ -856,7 +856,7 @@ struct Wide {
 // Many rows: the wavefronts have 32 rows each and go through the keys together.  Two tiles of 32 keys are converted to operands
 // once, K or V of one by each wavefront, into one of two stages in LDS, while the other is multiplied from: codes are converted
 // once for 128 rows, and a barrier stands behind 64 keys (behind 32, in 16x16x32 instructions, first visits of 4096 x 8 took 730 us
-// where 680).  Of their time 46 % are vector instructions and 30 % products.  Workgroups go to the 8
+// where 680).  Of their cycles 51 % are vector instructions, 35 % products.  Workgroups go to the 8
 // XCDs in turn, so that with the heads counted first the tiles of a (user, head) meet its keys in one XCD's L2 (8 heads), or two's.
 template <int D, typename T, Numbered N>
 __global__ __launch_bounds__(256, 2) void q8_attn_wide_kernel(Q8AttnArgs a) {
