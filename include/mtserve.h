@@ -357,7 +357,8 @@ int32_t mts_kv_append_q8(const mts_cache_desc* cache, int32_t layer, int32_t row
                          int64_t k_token_stride, const void* v_new, int64_t v_token_stride,
                          const mts_batch_meta* meta, void* stream);
 /* mts_kv_unpack and mts_kv_pack of an 8-bit pool: runs of rows [2][n][H][D] of row_dtype are quantised as they
- * are written, and read back as the values that their codes stand for (exact in either type). */
+ * are written, and read back as the values that their codes stand for (exact in either type).  A token that two
+ * runs of one unpack write gets the codes and exponents of either: they have to be the same rows. */
 int32_t mts_kv_unpack_q8(const mts_cache_desc* cache, int32_t layer, int32_t row_dtype, const void* staging,
                          int32_t num_segs, const int32_t* seg_user, const int32_t* seg_pos,
                          const int64_t* seg_tok_indptr, int32_t max_seg_tokens, const mts_batch_meta* meta,

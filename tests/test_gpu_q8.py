@@ -782,3 +782,34 @@ def test_pools_and_strides_beyond_32_bits():
         got.append([host(qo), host(out), host(back), image.cpu().numpy()])
     for a, b in zip(*got):
         np.testing.assert_array_equal(a, b)
+
+
+def test_the_same_run_twice_and_calls_side_by_side():
+    rng = np.random.default_rng(52)
+    H, G, D, S = 2, 2, 64, 16
+    s = Step(52, H, D, S, [45, 200], [1, 1], "bf16")
+    a, b = rows(rng, (2, 45, H, D), "bf16"), rows(rng, (2, 200, H, D), "bf16")
+    runs, data = [(0, 0, 45), (1, 0, 200), (0, 0, 45), (1, 10, 33)], [a, b, a, b[:, 10:43]]
+    s.unpack(runs, data)
+    R.store(s.image, s.w.user_pages(0), S, 0, a)
+    R.store(s.image, s.w.user_pages(1), S, 0, b)
+    np.testing.assert_array_equal(s.pool(), s.image)
+    for got, x in zip(s.pack(runs), data):
+        np.testing.assert_array_equal(host(got), R.quantise(x)[2])
+    # calls of two pools on two streams at once, each with a workspace of its own
+    steps = [Step(53 + i, H, D, S, p, n, "bf16") for i, (p, n) in enumerate((([5000, 30], [1, 2]), ([300, 2000], [150, 1])))]
+    work = []
+    for t in steps:
+        t.fill_prefixes(rng)
+        k, v, q = (dev(rows(rng, (t.w.total_new, h, D), "bf16"), "bf16") for h in (H, H, H * G))
+        t.append(k, v)
+        nb = mts.mts_attn_q8_workspace_bytes(t.cache.desc, H * G, t.batch.meta)
+        work.append((q, torch.empty(max(nb, 256), dtype=torch.uint8, device=DEV), nb, torch.cuda.Stream(), t.attention(q, G)))
+    outs = [torch.zeros_like(w[0]) for w in work]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for t, (q, ws, nb, stream, _), out in zip(steps, work, outs):
+            mts.mts_attn_incremental_q8(t.cache.desc, 0, B.MTS_BF16, H * G, q, out, t.batch.meta, 0.0, ws, nb, stream)
+    torch.cuda.synchronize()
+    for (_, _, _, _, alone), out in zip(work, outs):
+        np.testing.assert_array_equal(host(out), alone)
