@@ -1169,11 +1169,12 @@ Q8AttnPlan plan_q8_attention(const Q8Geom& g, int32_t num_q_heads, const BatchDe
     // 20.4 / 17.2, 5 of 9-20 K x 3 27.6 / 21.1, 29 of 0.4-2.6 K x 8 of 128 26.3 / 27.0, 44 of 4-12 K x 1 of 32 15.6 / 14.6, 50 of
     // 11-20 K x 8 82.7 / 77.5; 32 rows each behind 32 x 10 K x 8 of 128 159 / 146, 64 behind 111 x 3.7 K x 2 86.6 / 67.9.  With 1024
     // for 64 x 1.5 K x 8 of 64 28.3 where 27.4, for 32 x 10 K x 8 of 128 141 where 130, with 4096 135.  Short histories are not cut,
-    // which saves the second launch, nor is what fills the chip without: cut / not, 1 user's 900 keys x 8 heads 9.3 / 7.9, 40 users'
-    // 700 x 8 of 128 19.6 / 14.1, 100 of 0.4-1.1 K x 16 of 32 28.4 / 21.0, 70 of 1.7-3.5 K x 16 with 30 rows 84.6 / 66.3, 161 of
-    // 0.6-2.3 K x 8 of 64 with 5-55 rows 110.7 / 78.9, 172 of 0.3-2.3 K x 16 of 32 68.7 / 56.4; 70 of 1.2-7.8 K x 16 65.8 / 83.4.
+    // which saves the second launch and the workgroups' starts: what is short depends on how many tiles there are without cutting.
+    // Cut / not, 1 user's 900 keys x 8 heads 9.3 / 7.9, 15 users' 0.6-2.4 K x 2 10.6 / 14.7; 32 of 0.9-1.4 K x 16 of 32 17.9 / 12.1, 44 of
+    // 0.4-2.5 K x 8 of 64 23.6 / 17.7, 75 of 0.3-1.1 K x 2 of 128 with 45-90 rows 29.3 / 21.4, 36 of 0.6-3.5 K x 8 16.1 / 16.4; 161 of
+    // 0.6-2.3 K x 8 of 64 with 5-55 rows 110.7 / 78.9; from 2048 tiles on always, 172 of 0.3-2.3 K x 16 of 32 68.7 / 56.4.
     const int64_t pairs = (int64_t)l.q_tiles * g.H, uncut = b.batch * pairs;
-    if (uncut < 2048 && b.max_total_len > (uncut < 1024 ? 1024 : l.rows == 16 ? 2048 : 6144)) {
+    if (uncut < 2048 && b.max_total_len > (uncut < 200 ? 1024 : l.rows == 32 && uncut >= 1024 ? 6144 : 2816)) {
       const int64_t work = keys * pairs;
       int64_t most = 2048;
       if (!wide && work < 1 << 19) most = 512;
